@@ -221,13 +221,14 @@ def _plain_neighbours(ids, dists, table, temperature):
 
 
 def _plain_statistics(logits, temperature):
-    """-> scaled logits less their largest, exp of that, its sum and the log-sum-exp of the scaled logits."""
-    x = logits.float() / temperature
+    """-> the logits less their largest, divided by the temperature, exp of that, its sum, and what normalises a row: its
+    largest logit and the logarithm of the sum."""
+    x = logits.float()
     top = x.amax(dim=1, keepdim=True)
-    x -= top
+    x = (x - top) / temperature
     e = x.exp()
     total = e.sum(dim=1, keepdim=True)
-    return x, e, total, total.log() + top
+    return x, e, total, torch.cat([top, total.log()], dim=1)
 
 
 def _plain_best(values, top):
@@ -241,7 +242,7 @@ def _plain_best(values, top):
 def _plain_logprobs(state):
     case, logits = state["case"], state["logits"]
     top, targets = min(case["top"], case["vocab"]), state["targets"].long()[:, None]
-    x, e, total, lse = _plain_statistics(logits, case["temperature"])
+    x, e, total, norms = _plain_statistics(logits, case["temperature"])
     p = e / total
     logp = x - total.log()
     if case["k"]:
@@ -253,7 +254,7 @@ def _plain_logprobs(state):
         p.scatter_add_(1, torch.where(used, tokens, 0).long(), share)
         logp = p.log()
     entropy = -torch.where(p > 0, p * logp, 0.0).sum(dim=1)
-    out = {"logprobs": logp.gather(1, targets)[:, 0], "entropy": entropy, "lse": lse[:, 0]}
+    out = {"logprobs": logp.gather(1, targets)[:, 0], "entropy": entropy, "norms": norms}
     if top:
         best = _plain_best(p if case["k"] else logits.float(), top)
         best_logp = logp.gather(1, best)
@@ -264,7 +265,7 @@ def _plain_logprobs(state):
 
 def _plain_policy(state):
     temperature, targets = state["case"]["temperature"], state["targets"].long()[:, None]
-    x, e, total, lse = _plain_statistics(state["logits"], temperature)
+    x, e, total, _ = _plain_statistics(state["logits"], temperature)
     p = e / total
     logp = x - total.log()
     logprobs = logp.gather(1, targets)[:, 0]
@@ -326,20 +327,20 @@ def _own(state):
         top = min(case["top"], case["vocab"])
         got = ivfpq.ivfpq_token_logprobs(logits, state["targets"], top=top, temperature=temperature,
                                          neighbours=state.get("neighbours"), weight=state.get("weight", 0.0))
-        out = {"logprobs": got.logprobs, "entropy": got.entropy, "lse": got.lse}
+        out = {"logprobs": got.logprobs, "entropy": got.entropy, "norms": got.norms}
         if top:
             out.update(top_tokens=got.top_tokens, top_logprobs=got.top_logprobs)
         return out
     if op == "policy":
         got = ivfpq.ivfpq_token_logprobs(logits, state["targets"], temperature=temperature)
-        grad = ivfpq.ivfpq_token_logprobs_backward(logits, state["targets"], got.lse, got.entropy, state["grad_logprobs"],
+        grad = ivfpq.ivfpq_token_logprobs_backward(logits, state["targets"], got.norms, got.entropy, state["grad_logprobs"],
                                                    state["grad_entropy"], temperature=temperature)
         return got.logprobs, got.entropy, grad
     tokens, given = state["tokens"], state["given"]
     if case["one_call"]:
         return ivfpq.ivfpq_distill_topk_step(logits, tokens, given, state["row_grads"], temperature=temperature)
-    loss, lse = ivfpq.ivfpq_distill_topk(logits, tokens, given, temperature=temperature)
-    return loss, ivfpq.ivfpq_distill_topk_backward(logits, lse, tokens, given, state["row_grads"], temperature=temperature)
+    loss, norms = ivfpq.ivfpq_distill_topk(logits, tokens, given, temperature=temperature)
+    return loss, ivfpq.ivfpq_distill_topk_backward(logits, norms, tokens, given, state["row_grads"], temperature=temperature)
 
 
 def run(state):
@@ -432,7 +433,9 @@ def exact(case, seed):
         mixed.scatter_add_(1, tokens.clamp(min=0).long(), weight * torch.where(tokens >= 0, given.double().exp(), 0.0))
         logp = mixed.log()
     p = logp.exp()
-    out = {"logprobs": logp.gather(1, targets)[:, 0], "entropy": -torch.where(p > 0, p * logp, 0.0).sum(dim=1), "lse": lse[:, 0]}
+    most = z.amax(dim=1, keepdim=True)
+    out = {"logprobs": logp.gather(1, targets)[:, 0], "entropy": -torch.where(p > 0, p * logp, 0.0).sum(dim=1),
+           "norms": torch.cat([state["logits"].double().amax(dim=1, keepdim=True), (z - most).exp().sum(dim=1, keepdim=True).log()], dim=1)}
     top = min(case["top"], case["vocab"])
     if top:
         values, places = torch.sort(logp, dim=1, descending=True, stable=True)
