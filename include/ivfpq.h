@@ -260,6 +260,118 @@ int ivfpq_refine(const float* d_data, int64_t n_data, int32_t d, const float* d_
                  const int64_t* d_cand_ids, int32_t n_cand, int32_t k, int64_t* d_ids, float* d_dists,
                  void* hip_stream);
 
+/* ---- language models around a search: 8-bit products, neighbours' tokens, log-probabilities, distillation ----
+ *
+ * A search over hidden states finds the stored states nearest to a query, and each carries the token that followed it.
+ * These calls give the model's logits (a product of 8-bit rows), turn search results into a distribution over tokens,
+ * score tokens under the model's distribution or its mixture with the neighbours', and train a model towards a few
+ * listed tokens (the neighbours', or a teacher model's best).  None needs an index.
+ *
+ *  - Matrices have rows of contiguous values, `stride` values (not bytes) from one row to the next; pointers and
+ *    strides need the alignment of a value only, unless stated.  `dtype` is an ivfpq_values_dtype_t.  Logits and 16-bit
+ *    rows are widened to fp32; sums, maxima and statistics are fp32; a result in 16 bits is rounded once, to nearest.
+ *  - A call takes up to 2^23 rows of logits of up to 2^30 tokens.
+ *  - A token is an int32 in [0, vocab); any other value marks an unused place.
+ *  - With T = temperature, 1e-6 <= T <= 1e6, a row of logits x has the distribution p_v = exp((x_v - M)/T) / sum_u exp((x_u - M)/T),
+ *    M its largest logit.  A logit of -inf has p = 0; a logit of the type's lowest value is a number like any other.  A row
+ *    whose logits are all -inf has no distribution: p = 0 everywhere, entropy 0, gradient 0.  A row that holds a NaN or +inf
+ *    has NaN statistics, log-probabilities, losses and gradients.
+ *  - norms [n][2] fp32 of a row: M and log(sum_u exp((x_u - M)/T)); {-inf, -inf} of a row without a distribution.
+ *    What a backward call needs of the forward pass.
+ *  - Calls only enqueue work on hip_stream; a call for zero rows does nothing.  Results do not depend on timing: the
+ *    same inputs give the same bits.  Outputs must not overlap inputs, but a gradient may be written over its logits
+ *    (same pointer, dtype and stride). */
+typedef enum {
+    IVFPQ_VALUES_FP32 = 0,
+    IVFPQ_VALUES_FP16 = 1, /* IEEE binary16 */
+    IVFPQ_VALUES_BF16 = 2  /* the upper half of a binary32 */
+} ivfpq_values_dtype_t;
+
+enum {
+    IVFPQ_MAX_TOP = 128,     /* alternatives of ivfpq_token_logprobs */
+    IVFPQ_MAX_LISTED = 1024, /* listed tokens (neighbours, a teacher's) of a row */
+    IVFPQ_MAX_MIXED = 256,   /* alternatives and neighbours together, where both are asked for */
+    IVFPQ_MAX_Q8_K = 65536   /* components of an 8-bit row: sums of products stay within int32 */
+};
+
+/* Rows as signed 8-bit codes with a scale each: s = max_j |x_j| / 127 in fp32, code_j = x_j / s rounded to the nearest
+ * integer (ties to even), within [-127, 127]; s and the codes of a row of zeros are 0.  A row that holds a NaN or an
+ * infinity has s = NaN and codes 0.  d_rows [n][d]; d_codes [n][code_stride] int8, of which the codes [d, code_stride) of a
+ * row are written as 0, code_stride >= d; d_scales [n] fp32.  1 <= d <= IVFPQ_MAX_Q8_K. */
+int ivfpq_quantize_rows(const void* d_rows, int32_t dtype, int64_t n, int32_t d, int64_t row_stride, int8_t* d_codes,
+                        int64_t code_stride, float* d_scales, void* hip_stream);
+
+/* out[i][j] = (a_scale[i] * b_scale[j]) * sum_c a[i][c] b[j][c] + bias[j]: the product of 8-bit rows on the matrix cores,
+ * summed exactly in int32.  Hidden states (a) and an output embedding (b) give logits; queries and stored vectors give
+ * inner products, and with bias[j] = -|b_j|^2 / 2 the largest value of a row is its nearest stored vector.
+ *   d_a [m][k], d_b [n][k] int8: both pointers 16-byte aligned, both strides multiples of 16 and at least k rounded up to
+ *   16; every row's bytes up to there, the last row's too, are read, and those from k on ignored.  d_a_scales [m], d_b_scales [n], d_bias [n] (may be NULL) fp32.
+ *   d_out [m][n] of out_dtype, out_stride >= n.  1 <= k <= IVFPQ_MAX_Q8_K. */
+int ivfpq_q8_matmul(const int8_t* d_a, int64_t a_stride, const float* d_a_scales, int64_t m, const int8_t* d_b,
+                    int64_t b_stride, const float* d_b_scales, int64_t n, int32_t k, const float* d_bias, void* d_out,
+                    int32_t out_dtype, int64_t out_stride, void* hip_stream);
+
+/* Search results as a distribution over tokens: neighbour j weighs exp(-dist_j / temperature), the weights of a query sum
+ * to one, and neighbours with the same token add up.  d_ids [nq][k] i64 and d_dists [nq][k] fp32 as ivfpq_search returns
+ * them; d_id_tokens [n_ids] int32: the token of every id.  A neighbour whose id is outside [0, n_ids), whose distance is not
+ * finite or whose token is negative is left out.  d_tokens [nq][k] int32: the distinct tokens in the order of their first
+ * neighbour, d_logprobs [nq][k] fp32 their log-probabilities; unused places hold -1 and -inf.  1 <= k <= IVFPQ_MAX_LISTED, 1e-30 <= temperature <= 1e30. */
+int ivfpq_neighbour_tokens(const int64_t* d_ids, const float* d_dists, int64_t nq, int32_t k, const int32_t* d_id_tokens,
+                           int64_t n_ids, float temperature, int32_t* d_tokens, float* d_logprobs, void* hip_stream);
+
+/* Log-probability of one given token a row, entropy of the row's distribution and its `top` most likely tokens.
+ *   d_logits [n][vocab]                     d_targets [n] int32, may be NULL
+ *   d_logprobs [n]: of d_targets, 0 for a target outside [0, vocab); NULL if and only if d_targets is
+ *   d_entropy [n] (nats), d_norms [n][2]: may be NULL
+ *   d_top_tokens, d_top_logprobs [n][top]: descending, ties to the lower token; tokens with p = 0 are not listed, and unused
+ *   places hold -1 and -inf.  The order of the model's own distribution is that of the logits.  0 <= top <= IVFPQ_MAX_TOP.
+ * n_neighbours > 0 mixes the rows' distributions with listed ones (ivfpq_neighbour_tokens): (1 - weight) p + weight q,
+ * 0 < weight < 1, q given by d_neighbour_tokens and d_neighbour_logprobs [n][n_neighbours]; the used tokens of a row are
+ * distinct.  Log-probabilities, entropy and alternatives are then the mixture's (norms stay the model's).  A row without
+ * a used neighbour is the model's alone, a row whose logits are all -inf the neighbours' alone.
+ * 0 <= n_neighbours <= IVFPQ_MAX_LISTED; where top > 0 and n_neighbours > 0, top + n_neighbours <= IVFPQ_MAX_MIXED.
+ * d_workspace: >= ivfpq_token_logprobs_workspace_bytes(...) (may be 0), 256-byte aligned. */
+size_t ivfpq_token_logprobs_workspace_bytes(int64_t n, int32_t vocab, int32_t top, int32_t n_neighbours);
+int ivfpq_token_logprobs(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab, int64_t row_stride,
+                         const int32_t* d_targets, float temperature, int32_t top, const int32_t* d_neighbour_tokens,
+                         const float* d_neighbour_logprobs, int32_t n_neighbours, float weight, float* d_logprobs,
+                         float* d_entropy, float* d_norms, int32_t* d_top_tokens, float* d_top_logprobs, void* d_workspace,
+                         size_t workspace_bytes, void* hip_stream);
+
+/* Gradient with respect to the logits of sum_i g_i logprob_i + h_i entropy_i (the model's own distribution, no
+ * mixture), g = d_grad_logprobs [n], h = d_grad_entropy [n]; either may be NULL (zeros), not both:
+ *   grad[v] = (g (v == target) - g p_v - h p_v (log p_v + entropy)) / T,  g of a target outside [0, vocab) counted as 0.
+ * d_norms, d_entropy: of the forward call on the same logits, targets and temperature (d_entropy may be NULL without
+ * d_grad_entropy, d_targets without d_grad_logprobs).  d_grad [n][vocab] of the logits' dtype. */
+int ivfpq_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab, int64_t row_stride,
+                                  const int32_t* d_targets, float temperature, const float* d_norms, const float* d_entropy,
+                                  const float* d_grad_logprobs, const float* d_grad_entropy, void* d_grad,
+                                  int64_t grad_stride, void* hip_stream);
+
+/* Divergence of a student from a teacher of whom only a few tokens a row are known: with P the softmax of the listed
+ * teacher_logits / T (log-probabilities serve as well) and p the student's distribution over the whole vocabulary,
+ *   loss = T^2 sum_j P_j (log P_j - log p_token(j)).
+ * d_teacher_tokens [n][k] int32, d_teacher_logits [n][k] fp32; entries outside [0, vocab) or at -inf are unused, entries of
+ * the same token add up.  d_loss [n]: 0 without a used entry, +inf where the student gives one of them p = 0.
+ * d_norms [n][2].  1 <= k <= IVFPQ_MAX_LISTED.  d_workspace: >= ivfpq_distill_topk_workspace_bytes(n, vocab), 256-byte aligned. */
+size_t ivfpq_distill_topk_workspace_bytes(int64_t n, int32_t vocab);
+int ivfpq_distill_topk(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab, int64_t row_stride,
+                       const int32_t* d_teacher_tokens, const float* d_teacher_logits, int32_t k, float temperature,
+                       float* d_loss, float* d_norms, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradient of sum_i w_i loss_i with respect to the logits: grad[v] = T w (p_v - P_v), 0 in rows without a used entry.
+ * d_norms of the forward call; w = d_row_grads [n], NULL for ones.  d_grad [n][vocab] of the logits' dtype. */
+int ivfpq_distill_topk_backward(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab, int64_t row_stride,
+                                const float* d_norms, const int32_t* d_teacher_tokens, const float* d_teacher_logits,
+                                int32_t k, float temperature, const float* d_row_grads, void* d_grad, int64_t grad_stride,
+                                void* hip_stream);
+
+/* Both in one call, for training steps whose row weights are known beforehand.  Workspace as ivfpq_distill_topk. */
+int ivfpq_distill_topk_step(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab, int64_t row_stride,
+                            const int32_t* d_teacher_tokens, const float* d_teacher_logits, int32_t k, float temperature,
+                            const float* d_row_grads, float* d_loss, void* d_grad, int64_t grad_stride, void* d_workspace,
+                            size_t workspace_bytes, void* hip_stream);
+
 /* ---- measurement aid ---- */
 
 /* When enabled, search calls record HIP events around their stages on the stream they run on (the events

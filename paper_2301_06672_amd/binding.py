@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import numpy as np
 import torch  # imported before the library so that both share one HIP runtime
@@ -25,6 +25,9 @@ MAX_PROBES = 1024
 STATIC_SCRATCH_BYTES = 64 << 20
 TUNE_SCAN_THREADS, TUNE_ORDER_BLOCK, TUNE_SCAN_SHARE, TUNE_EARLY_EXIT, TUNE_LDS_PAD, TUNE_SCAN_ROUTE = 0, 1, 2, 3, 4, 5
 
+MAX_TOP, MAX_LISTED, MAX_MIXED, MAX_Q8_K = 128, 1024, 256, 65536
+VALUES_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
 OK, EINVAL, ENOSPACE, EHIP, EUNSUPPORTED, ESTATE = 0, -1, -2, -3, -4, -5
 
 # every symbol include/ivfpq.h declares
@@ -35,6 +38,9 @@ EXPORTS = (
     "ivfpq_device_bytes", "ivfpq_upload", "ivfpq_search_workspace_bytes", "ivfpq_search", "ivfpq_search_static",
     "ivfpq_select_probes", "ivfpq_search_with_probes", "ivfpq_dump_lut", "ivfpq_scan_list", "ivfpq_refine",
     "ivfpq_set_stage_timing", "ivfpq_stage_times_ms", "ivfpq_scan_kernel_info", "ivfpq_stream_read", "ivfpq_last_error",
+    "ivfpq_quantize_rows", "ivfpq_q8_matmul", "ivfpq_neighbour_tokens", "ivfpq_token_logprobs_workspace_bytes",
+    "ivfpq_token_logprobs", "ivfpq_token_logprobs_backward", "ivfpq_distill_topk_workspace_bytes", "ivfpq_distill_topk",
+    "ivfpq_distill_topk_backward", "ivfpq_distill_topk_step",
 )
 
 
@@ -97,6 +103,20 @@ def _declare(L):
     L.ivfpq_stage_times_ms.argtypes = [vp, c.POINTER(c.c_float * 8)]
     L.ivfpq_scan_kernel_info.argtypes = [vp, i32, c.c_char_p, sz]
     L.ivfpq_stream_read.argtypes = [vp, sz, vp, i32, vp]
+    f32 = c.c_float
+    logits = [vp, i32, i64, i32, i64]
+    L.ivfpq_quantize_rows.argtypes = [vp, i32, i64, i32, i64, vp, i64, vp, vp]
+    L.ivfpq_q8_matmul.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, vp, i32, i64, vp]
+    L.ivfpq_neighbour_tokens.argtypes = [vp, vp, i64, i32, vp, i64, f32, vp, vp, vp]
+    L.ivfpq_token_logprobs_workspace_bytes.argtypes = [i64, i32, i32, i32]
+    L.ivfpq_token_logprobs_workspace_bytes.restype = sz
+    L.ivfpq_token_logprobs.argtypes = logits + [vp, f32, i32, vp, vp, i32, f32, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.ivfpq_token_logprobs_backward.argtypes = logits + [vp, f32, vp, vp, vp, vp, vp, i64, vp]
+    L.ivfpq_distill_topk_workspace_bytes.argtypes = [i64, i32]
+    L.ivfpq_distill_topk_workspace_bytes.restype = sz
+    L.ivfpq_distill_topk.argtypes = logits + [vp, vp, i32, f32, vp, vp, vp, sz, vp]
+    L.ivfpq_distill_topk_backward.argtypes = logits + [vp, vp, vp, i32, f32, vp, vp, i64, vp]
+    L.ivfpq_distill_topk_step.argtypes = logits + [vp, vp, i32, f32, vp, vp, vp, i64, vp, sz, vp]
     L.ivfpq_last_error.restype = c.c_char_p
     for name in EXPORTS:
         fn = getattr(L, name)
@@ -164,6 +184,215 @@ def ivfpq_stream_read(buf: torch.Tensor, n_out: int = 8192) -> torch.Tensor:
     out = torch.empty(n_out, dtype=torch.int32, device="cuda")
     _check(lib().ivfpq_stream_read(_dp(buf), buf.numel() * buf.element_size(), _dp(out), int(n_out), _stream()))
     return out
+
+
+# ---- language models around a search.  Inputs are CUDA tensors on the current device; rows may have any stride, the values
+# of a row are contiguous.
+
+class TokenLogprobs(NamedTuple):
+    logprobs: Optional[torch.Tensor]       # [n] of the targets; None without targets
+    entropy: torch.Tensor                  # [n]
+    norms: torch.Tensor                    # [n][2], for the backward call
+    top_tokens: Optional[torch.Tensor]     # [n][top] int32, None with top = 0
+    top_logprobs: Optional[torch.Tensor]   # [n][top]
+
+
+def _need(ok: bool, message: str):
+    if not ok:
+        raise IvfpqError(EINVAL, message)
+
+
+def _on_device(what: str, *tensors):
+    device = torch.cuda.current_device()
+    for t in tensors:
+        _need(t is None or (isinstance(t, torch.Tensor) and t.is_cuda and t.device.index == device),
+              f"{what}: a tensor is not on the current CUDA device")
+
+
+def _plain(what: str, t: torch.Tensor, dtype, shape):
+    """A contiguous tensor of this type and shape."""
+    _need(t.dtype == dtype and tuple(t.shape) == tuple(shape), f"{what}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t.contiguous()
+
+
+def _value_rows(what: str, x: torch.Tensor) -> torch.Tensor:
+    _need(x.dim() == 2 and x.dtype in VALUES_DTYPES, f"{what}: expected a matrix of float32, float16 or bfloat16, got {x.dtype} {tuple(x.shape)}")
+    n, d = x.shape
+    return x if (d <= 1 or x.stride(1) == 1) and (n <= 1 or x.stride(0) >= d) else x.contiguous()
+
+
+def _grad_like(what: str, logits: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
+    if out is None:
+        return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    _on_device(what, out)
+    n, d = logits.shape
+    _need(out.shape == logits.shape and out.dtype == logits.dtype and (d <= 1 or out.stride(1) == 1) and (n <= 1 or out.stride(0) >= d),
+          f"{what}: out has another shape, type or layout than the logits")
+    return out
+
+
+def _listed(what: str, tokens: torch.Tensor, values: torch.Tensor, n: int):
+    _need(tokens.dim() == 2, f"{what}: listed tokens are a matrix")
+    shape = (n, tokens.shape[1])
+    return _plain(what, tokens, torch.int32, shape), _plain(what, values, torch.float32, shape)
+
+
+def _scratch(nbytes: int) -> Optional[torch.Tensor]:
+    return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+
+
+def _logits(x: torch.Tensor):
+    return _dp(x), VALUES_DTYPES[x.dtype], x.shape[0], x.shape[1], x.stride(0)
+
+
+def ivfpq_quantize_rows(rows: torch.Tensor):
+    """-> (codes int8 [n][d], scales fp32 [n]); the codes' rows lie a multiple of 16 bytes apart, zeros in between."""
+    _on_device("ivfpq_quantize_rows", rows)
+    x = _value_rows("ivfpq_quantize_rows", rows)
+    n, d = x.shape
+    codes = torch.empty((n, -(-d // 16) * 16), dtype=torch.int8, device="cuda")
+    scales = torch.empty(n, dtype=torch.float32, device="cuda")
+    _check(lib().ivfpq_quantize_rows(_dp(x), VALUES_DTYPES[x.dtype], n, d, x.stride(0), _dp(codes), codes.shape[1], _dp(scales), _stream()))
+    return codes[:, :d], scales
+
+
+def _code_rows(what: str, codes: torch.Tensor):
+    """-> (codes, row stride): rows of 16-byte pieces that can all be read, as ivfpq_quantize_rows makes them; other layouts are copied."""
+    _need(codes.dim() == 2 and codes.dtype == torch.int8, f"{what}: codes are a matrix of int8, got {codes.dtype} {tuple(codes.shape)}")
+    n, k = codes.shape
+    width = -(-k // 16) * 16
+    stride = codes.stride(0) if n > 1 else width
+    fits = (k <= 1 or codes.stride(1) == 1) and stride % 16 == 0 and stride >= width and codes.data_ptr() % 16 == 0 and (
+        codes.storage_offset() + (n - 1) * stride + width <= codes.untyped_storage().nbytes())
+    if n == 0 or fits:
+        return codes, max(stride, width)
+    padded = torch.zeros((n, width), dtype=torch.int8, device=codes.device)
+    padded[:, :k] = codes
+    return padded, width
+
+
+def ivfpq_q8_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.Tensor, b_scales: torch.Tensor, bias=None,
+                    out_dtype=torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """-> [m][n]: a_scales[i] * b_scales[j] * (a_codes[i] . b_codes[j]) + bias[j]."""
+    what = "ivfpq_q8_matmul"
+    _on_device(what, a_codes, a_scales, b_codes, b_scales, bias, out)
+    a, a_stride = _code_rows(what, a_codes)
+    b, b_stride = _code_rows(what, b_codes)
+    (m, k), n = a_codes.shape, b_codes.shape[0]
+    _need(b_codes.shape[1] == k, f"{what}: rows of {k} and {b_codes.shape[1]} codes")
+    sa, sb = _plain(what, a_scales, torch.float32, (m,)), _plain(what, b_scales, torch.float32, (n,))
+    bias = None if bias is None else _plain(what, bias, torch.float32, (n,))
+    if out is None:
+        _need(out_dtype in VALUES_DTYPES, f"{what}: out_dtype {out_dtype}")
+        out = torch.empty((m, n), dtype=out_dtype, device="cuda")
+    _need(out.shape == (m, n) and out.dtype in VALUES_DTYPES and (n <= 1 or out.stride(1) == 1), f"{what}: out has another shape, type or layout")
+    _check(lib().ivfpq_q8_matmul(_dp(a), a_stride, _dp(sa), m, _dp(b), b_stride, _dp(sb), n, k, _dp(bias), _dp(out),
+                                 VALUES_DTYPES[out.dtype], out.stride(0), _stream()))
+    return out
+
+
+def ivfpq_neighbour_tokens(ids: torch.Tensor, dists: torch.Tensor, id_tokens: torch.Tensor, temperature: float):
+    """-> (tokens int32 [nq][k], log-probabilities fp32 [nq][k]) of search results; id_tokens [n_ids] int32 is the token of every id."""
+    what = "ivfpq_neighbour_tokens"
+    _on_device(what, ids, dists, id_tokens)
+    _need(ids.dim() == 2, f"{what}: ids are a matrix")
+    nq, k = ids.shape
+    ids, dists = _plain(what, ids, torch.int64, (nq, k)), _plain(what, dists, torch.float32, (nq, k))
+    table = _plain(what, id_tokens, torch.int32, (id_tokens.numel(),))
+    tokens = torch.empty((nq, k), dtype=torch.int32, device="cuda")
+    logprobs = torch.empty((nq, k), dtype=torch.float32, device="cuda")
+    _check(lib().ivfpq_neighbour_tokens(_dp(ids), _dp(dists), nq, k, _dp(table), table.numel(), temperature, _dp(tokens), _dp(logprobs), _stream()))
+    return tokens, logprobs
+
+
+def ivfpq_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 0, temperature: float = 1.0,
+                         neighbours=None, weight: float = 0.0) -> TokenLogprobs:
+    """Log-probabilities of `targets` (int32 [n]), entropy and the `top` best tokens of rows of logits; neighbours: (tokens,
+    log-probabilities) as ivfpq_neighbour_tokens gives them, mixed in with this weight."""
+    what = "ivfpq_token_logprobs"
+    _on_device(what, logits, targets, *(neighbours or ()))
+    x = _value_rows(what, logits)
+    n, vocab = x.shape
+    targets = None if targets is None else _plain(what, targets, torch.int32, (n,))
+    near_tokens, near_logprobs = (None, None) if neighbours is None else _listed(what, *neighbours, n)
+    k = 0 if near_tokens is None else near_tokens.shape[1]
+    logprobs = None if targets is None else torch.empty(n, dtype=torch.float32, device="cuda")
+    entropy = torch.empty(n, dtype=torch.float32, device="cuda")
+    norms = torch.empty((n, 2), dtype=torch.float32, device="cuda")
+    best = (torch.empty((n, top), dtype=torch.int32, device="cuda"), torch.empty((n, top), dtype=torch.float32, device="cuda")) if top > 0 else (None, None)
+    need = lib().ivfpq_token_logprobs_workspace_bytes(n, vocab, top, k)
+    ws = _scratch(need)
+    _check(lib().ivfpq_token_logprobs(*_logits(x), _dp(targets), temperature, top, _dp(near_tokens), _dp(near_logprobs), k, weight,
+                                      _dp(logprobs), _dp(entropy), _dp(norms), _dp(best[0]), _dp(best[1]), _dp(ws), need, _stream()))
+    return TokenLogprobs(logprobs, entropy, norms, *best)
+
+
+def ivfpq_token_logprobs_backward(logits: torch.Tensor, targets: Optional[torch.Tensor], norms: torch.Tensor, entropy: Optional[torch.Tensor],
+                                  grad_logprobs: Optional[torch.Tensor], grad_entropy: Optional[torch.Tensor] = None,
+                                  temperature: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """-> the gradient with respect to the logits (written to `out`, which may be the logits themselves)."""
+    what = "ivfpq_token_logprobs_backward"
+    _on_device(what, logits, targets, norms, entropy, grad_logprobs, grad_entropy)
+    x = _value_rows(what, logits)
+    n = x.shape[0]
+    row = lambda t, dtype=torch.float32: None if t is None else _plain(what, t, dtype, (n,))
+    targets, entropy, by_logprob, by_entropy = row(targets, torch.int32), row(entropy), row(grad_logprobs), row(grad_entropy)
+    norms = _plain(what, norms, torch.float32, (n, 2))
+    grad = _grad_like(what, x, out)
+    _check(lib().ivfpq_token_logprobs_backward(*_logits(x), _dp(targets), temperature, _dp(norms), _dp(entropy), _dp(by_logprob),
+                                               _dp(by_entropy), _dp(grad), grad.stride(0), _stream()))
+    return grad
+
+
+def ivfpq_distill_topk(logits: torch.Tensor, teacher_tokens: torch.Tensor, teacher_logits: torch.Tensor, temperature: float = 1.0):
+    """-> (loss fp32 [n], norms [n][2]): divergence of the rows' distributions from a teacher's listed tokens."""
+    what = "ivfpq_distill_topk"
+    _on_device(what, logits, teacher_tokens, teacher_logits)
+    x = _value_rows(what, logits)
+    n, vocab = x.shape
+    tokens, values = _listed(what, teacher_tokens, teacher_logits, n)
+    loss = torch.empty(n, dtype=torch.float32, device="cuda")
+    norms = torch.empty((n, 2), dtype=torch.float32, device="cuda")
+    need = lib().ivfpq_distill_topk_workspace_bytes(n, vocab)
+    ws = _scratch(need)
+    _check(lib().ivfpq_distill_topk(*_logits(x), _dp(tokens), _dp(values), tokens.shape[1], temperature, _dp(loss), _dp(norms), _dp(ws),
+                                    need, _stream()))
+    return loss, norms
+
+
+def ivfpq_distill_topk_backward(logits: torch.Tensor, norms: torch.Tensor, teacher_tokens: torch.Tensor, teacher_logits: torch.Tensor,
+                                row_grads: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """-> the gradient of sum(row_grads * loss) with respect to the logits (written to `out`, which may be the logits themselves)."""
+    what = "ivfpq_distill_topk_backward"
+    _on_device(what, logits, norms, teacher_tokens, teacher_logits, row_grads)
+    x = _value_rows(what, logits)
+    n = x.shape[0]
+    tokens, values = _listed(what, teacher_tokens, teacher_logits, n)
+    norms = _plain(what, norms, torch.float32, (n, 2))
+    row_grads = None if row_grads is None else _plain(what, row_grads, torch.float32, (n,))
+    grad = _grad_like(what, x, out)
+    _check(lib().ivfpq_distill_topk_backward(*_logits(x), _dp(norms), _dp(tokens), _dp(values), tokens.shape[1], temperature, _dp(row_grads),
+                                             _dp(grad), grad.stride(0), _stream()))
+    return grad
+
+
+def ivfpq_distill_topk_step(logits: torch.Tensor, teacher_tokens: torch.Tensor, teacher_logits: torch.Tensor,
+                            row_grads: Optional[torch.Tensor] = None, temperature: float = 1.0, out: Optional[torch.Tensor] = None):
+    """-> (loss [n], gradient): ivfpq_distill_topk and its backward call in one."""
+    what = "ivfpq_distill_topk_step"
+    _on_device(what, logits, teacher_tokens, teacher_logits, row_grads)
+    x = _value_rows(what, logits)
+    n, vocab = x.shape
+    tokens, values = _listed(what, teacher_tokens, teacher_logits, n)
+    row_grads = None if row_grads is None else _plain(what, row_grads, torch.float32, (n,))
+    loss = torch.empty(n, dtype=torch.float32, device="cuda")
+    grad = _grad_like(what, x, out)
+    need = lib().ivfpq_distill_topk_workspace_bytes(n, vocab)
+    ws = _scratch(need)
+    _check(lib().ivfpq_distill_topk_step(*_logits(x), _dp(tokens), _dp(values), tokens.shape[1], temperature, _dp(row_grads), _dp(loss),
+                                         _dp(grad), grad.stride(0), _dp(ws), need, _stream()))
+    return loss, grad
 
 
 class Index:

@@ -23,8 +23,9 @@ HIP_FLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 # (object, source, flags): search, the matrix-core filter of its scan and the sums of what that lists, the scan of groups of
-# pairs (one object per table dtype each), index construction
+# pairs (one object per table dtype each), index construction; log-probabilities and distillation, neighbours' tokens, 8-bit products
 DEVICE_OBJECTS = [("ivfpq_device", "ivfpq_device", []), ("ivfpq_build", "ivfpq_build", []), ("ivfpq_scan_filter", "ivfpq_scan_filter", []),
+                  ("ivfpq_logits", "ivfpq_logits", []), ("ivfpq_neighbours", "ivfpq_neighbours", []), ("ivfpq_q8", "ivfpq_q8", []),
                   *((f"ivfpq_candidates_{lut}", "ivfpq_candidates", [f"-DIVFPQ_CANDIDATE_LUT={lut}"]) for lut in range(4)),
                   *((f"ivfpq_scan_group_{lut}", "ivfpq_scan_group", [f"-DIVFPQ_GROUP_LUT={lut}"]) for lut in range(4))]
 HOST_FLAGS = ["-O3", "-std=c++17", "-fPIC", "-fopenmp", "-mavx2", "-mfma", "-Wall"]

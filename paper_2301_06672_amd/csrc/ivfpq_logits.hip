@@ -1,0 +1,960 @@
+// Log-probabilities of tokens, the entropy and the best alternatives of rows of logits, mixed with listed tokens or not, the
+// loss towards a teacher's listed tokens, and the gradients of all of these.
+//
+// Everything a row needs is a sum over exp2(t), t = (x - M) log2(e) / T with M the row's largest logit:
+//   S = sum 2^t,  U = sum t 2^t,   log p_v = ln2 (t_v - log2 S),   entropy = ln2 (log2 S - U / S).
+// Both terms of the entropy are non-negative (t <= 0), so nothing cancels.  Partial results (m, s, u) about an own maximum m
+// combine by shifting: s 2^d, (u + d s) 2^d, d = (m - M) log2(e) / T.  One pass over the logits is enough, and a row can be
+// split between workgroups.  x - M is formed before the scale, which keeps masks of the type's lowest value finite.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "ivfpq_float_key.hpp"
+#include "ivfpq_hip_util.hpp"
+#include "ivfpq_values.hpp"
+
+using namespace ivfpq;
+
+namespace {
+
+constexpr int kRowThreads = 256, kRowWaves = kRowThreads / 64;
+constexpr int kMostSplits = 64;                            // workgroups that share a row
+constexpr int kMostTop = IVFPQ_MAX_MIXED;                  // keys a selection keeps
+constexpr int kCandidates = 2048 - kMostTop;               // ... and takes in before it sorts
+constexpr float kLeastPower = -150.f;                      // 2^t is 0 in fp32 below this: t is cut there before t 2^t
+
+struct Partial { float m, s, u, unused; };
+
+// ---- statistics
+
+struct RowSum {
+    float m = -INFINITY, s = 0.f, u = 0.f;
+    RowSum() = default;
+    __device__ explicit RowSum(const Partial& p) : m(p.m), s(p.s), u(p.u) {}
+    // makes `most` the reference of the sums; most >= m
+    __device__ inline void raise(float most, float scale) {
+        const bool none = m == -INFINITY;
+        const float d = none ? 0.f : (m - most) * scale;
+        const float f = none ? 0.f : exp2_fast(d);
+        u = __builtin_fmaf(fmaxf(d, kLeastPower), s, u) * f;
+        s *= f;                                            // a NaN stays one
+        m = most;
+    }
+    __device__ inline void join(RowSum b, float scale) {
+        const float most = fmaxf(m, b.m);
+        if (most == -INFINITY) {                           // nothing yet, or nothing but NaN
+            s += b.s;
+            u += b.u;
+            return;
+        }
+        raise(most, scale);
+        b.raise(most, scale);
+        s += b.s;
+        u += b.u;
+    }
+};
+
+__device__ inline RowSum wave_join(RowSum a, float scale) {
+    for (int off = 32; off; off >>= 1) {
+        RowSum b;
+        b.m = __shfl_xor(a.m, off);
+        b.s = __shfl_xor(a.s, off);
+        b.u = __shfl_xor(a.u, off);
+        // the lower lane's part first in both, so that both get the same bits
+        if (threadIdx.x & off) { const RowSum t = a; a = b; b = t; }
+        a.join(b, scale);
+    }
+    return a;
+}
+
+// ---- the largest keys of a row
+
+// A key orders logits descending and, among equal ones, tokens ascending; keys of a row are distinct.  0: none.
+__device__ inline uint64_t token_key(float x, uint32_t token) {
+    return ((uint64_t)ordered_key(x + 0.f) << 32) | (uint32_t)~token;      // -0 counts as +0
+}
+__device__ inline float key_value(uint64_t key) { return ordered_key_value((uint32_t)(key >> 32)); }
+__device__ inline int key_token(uint64_t key) { return (int)~(uint32_t)key; }
+
+struct Selection {
+    uint64_t found[kCandidates + kMostTop];    // candidates, then room for the kept ones
+    uint64_t kept[kMostTop];                   // the largest so far, descending
+    uint64_t wave_bound[2][kRowWaves];
+    int n_found;
+};
+
+// found[0, n) descending, n a power of two
+__device__ inline void sort_found(Selection& sel, int n) {
+    for (int len = 2; len <= n; len <<= 1)
+        for (int step = len >> 1; step; step >>= 1) {
+            for (int i = threadIdx.x; i < n / 2; i += kRowThreads) {
+                const int a = 2 * i - (i & (step - 1)), b = a + step;
+                const uint64_t x = sel.found[a], y = sel.found[b];
+                if ((x < y) == ((a & len) == 0)) { sel.found[a] = y; sel.found[b] = x; }
+            }
+            __syncthreads();
+        }
+}
+
+__device__ inline int power_of_two(int n) { return n <= 1 ? 1 : 1 << (32 - __clz(n - 1)); }
+
+// The `want` largest of found[0, n) and kept[0, n_kept) become the kept ones; returns how many there are.  Few keys find their
+// places by counting the larger ones, many are sorted.  Starts after a barrier and ends with one.
+__device__ inline int keep_best(Selection& sel, int n, int n_kept, int want) {
+    const int tid = threadIdx.x;
+    for (int i = tid; i < n_kept; i += kRowThreads) sel.found[n + i] = sel.kept[i];
+    const int total = n + n_kept;
+    const int keep = total < want ? total : want;
+    if (total <= 2 * kRowThreads) {
+        __syncthreads();
+        for (int i = tid; i < total; i += kRowThreads) {
+            const uint64_t mine = sel.found[i];
+            int place = 0;
+            for (int j = 0; j < total; ++j) {
+                const uint64_t other = sel.found[j];
+                place += other > mine || (other == mine && j < i);
+            }
+            if (place < want) sel.kept[place] = mine;      // the barrier above: kept has been copied
+        }
+    } else {
+        const int padded = power_of_two(total);
+        for (int i = total + tid; i < padded; i += kRowThreads) sel.found[i] = 0;
+        __syncthreads();
+        sort_found(sel, padded);
+        for (int i = tid; i < keep; i += kRowThreads) sel.kept[i] = sel.found[i];
+    }
+    if (tid == 0) sel.n_found = 0;
+    __syncthreads();
+    return keep;
+}
+
+// Adds what `scan` finds to the kept keys.  scan(bound, push) calls push(key) for its keys >= bound, each at most once.  More than
+// fit raise the bound to the want-th of those that did (keys below it cannot be among the best) and are looked for
+// again; at least kCandidates - want keys are ruled out each time, so this ends.
+// n_found is 0 on entry, and is on return; no wave is past the last barrier's reads.
+template <class Scan>
+__device__ inline int take_candidates(Selection& sel, uint64_t& bound, int n_kept, int want, Scan&& scan) {
+    for (;;) {
+        scan(bound, [&](uint64_t key) {
+            const int at = atomicAdd(&sel.n_found, 1);     // the order of arrival does not matter: keys are sorted
+            if (at < kCandidates) sel.found[at] = key;
+        });
+        __syncthreads();
+        const int n = sel.n_found;
+        __syncthreads();
+        if (n == 0) return n_kept;
+        if (n <= kCandidates) {
+            n_kept = keep_best(sel, n, n_kept, want);
+            if (n_kept == want && sel.kept[want - 1] > bound) bound = sel.kept[want - 1];
+            return n_kept;
+        }
+        for (int i = kCandidates + threadIdx.x; i < 2048; i += kRowThreads) sel.found[i] = 0;
+        if (threadIdx.x == 0) sel.n_found = 0;
+        __syncthreads();
+        sort_found(sel, 2048);
+        if (sel.found[want - 1] > bound) bound = sel.found[want - 1];
+        __syncthreads();
+    }
+}
+
+// A lower bound of the want-th largest key of a workgroup, from one key of each lane (its largest, 0 if it has none).
+// Either holds: with q = ceil(want / waves), every wave has q keys that are at least the smallest of the waves' q-th; and a
+// wave has `want` keys that are at least its want-th.
+__device__ inline uint64_t bound_of_best(Selection& sel, uint64_t mine, int want) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int larger = 0;
+    for (int j = 0; j < 64; ++j) {
+        const uint64_t other = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), j) << 32) |
+                               (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, j);
+        larger += other > mine;
+    }
+    if (lane == 0) sel.wave_bound[0][wave] = sel.wave_bound[1][wave] = 0;
+    __builtin_amdgcn_wave_barrier();
+    const int q = (want + kRowWaves - 1) / kRowWaves;
+    if (larger == q - 1) sel.wave_bound[0][wave] = mine;         // lanes without a key share a place and a value, 0
+    if (larger == want - 1) sel.wave_bound[1][wave] = mine;
+    __syncthreads();
+    uint64_t low = sel.wave_bound[0][0], high = sel.wave_bound[1][0];
+#pragma unroll
+    for (int w = 1; w < kRowWaves; ++w) {
+        low = sel.wave_bound[0][w] < low ? sel.wave_bound[0][w] : low;
+        high = sel.wave_bound[1][w] > high ? sel.wave_bound[1][w] : high;
+    }
+    __syncthreads();
+    return low > high ? low : high;
+}
+
+// ---- what is done with a row's statistics
+
+struct Listed {                       // tokens listed for every row, with a number each
+    const int32_t* tokens;            // [n][k]
+    const float* values;
+    int k;
+};
+
+struct RowsIn {
+    const void* data;
+    long long stride;
+    int vocab;
+    float temperature, scale;         // scale = log2(e) / T
+};
+
+struct ScoreOut {
+    const int32_t* targets;
+    Listed near;
+    float log_model, log_near;        // log(1 - weight), log(weight)
+    int top, want;                    // want: keys to select, top plus the neighbours that may be among them
+    float *logprobs, *entropy, *norms;
+    int32_t* top_tokens;
+    float* top_logprobs;
+};
+
+struct DistillOut {
+    Listed teacher;
+    float *loss, *norms;
+};
+
+struct MixShared {
+    int token[IVFPQ_MAX_LISTED];
+    float logp[IVFPQ_MAX_LISTED];     // of the mixture
+    double sums[kRowWaves];
+    float hit, model, near;           // the target's log-probability if it is listed; log weights in this row
+};
+
+// log(exp(a) + exp(b))
+__device__ inline float log_add(float a, float b) {
+    if (a != a || b != b) return a + b;
+    const float most = fmaxf(a, b), least = fminf(a, b);
+    if (most == -INFINITY) return most;
+    return most + log1pf(expf(least - most));
+}
+
+__device__ inline void write_norms(float* norms, long long row, float m, float log_s, bool none) {
+    if (!norms) return;
+    norms[2 * row] = none ? -INFINITY : (log_s != log_s ? log_s : m);
+    norms[2 * row + 1] = none ? -INFINITY : log_s;
+}
+
+// All threads of a workgroup, on the statistics of one row; kept: its `n_kept` largest keys (TOP).
+template <class T, bool TOP>
+__device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long long row, RowSum sum, int n_kept, Selection* sel, MixShared& mix) {
+    const int tid = threadIdx.x;
+    const T* x = reinterpret_cast<const T*>(in.data) + row * in.stride;
+    const bool none = sum.s == 0.f;                        // no logit above -inf (a largest one would have added 1)
+    const float log_s = logf(sum.s);
+    // log p of a logit
+    auto model_logp = [&](float v) { return none ? -INFINITY : (v - sum.m) / in.temperature - log_s; };
+    float entropy = none ? 0.f : log_s - kLn2 * (sum.u / sum.s);
+    const int target = out.targets && tid == 0 ? out.targets[row] : -1;
+    const bool wanted = target >= 0 && target < in.vocab;
+    if (tid == 0) write_norms(out.norms, row, sum.m, log_s, none);
+
+    if (out.near.k == 0) {
+        if (tid == 0) {
+            if (out.targets) out.logprobs[row] = wanted ? model_logp((float)x[target]) : 0.f;
+            if (out.entropy) out.entropy[row] = entropy;
+        }
+        if constexpr (TOP)
+            for (int i = tid; i < out.top; i += kRowThreads) {
+                const bool used = i < n_kept;
+                out.top_tokens[row * out.top + i] = used ? key_token(sel->kept[i]) : -1;
+                out.top_logprobs[row * out.top + i] = used ? model_logp(key_value(sel->kept[i])) : -INFINITY;
+            }
+        return;
+    }
+
+    // The mixture: m_v = (1 - w) p_v + w q_v differs from (1 - w) p_v at the listed tokens only, so its entropy is that of
+    // the scaled model with the listed terms exchanged (summed in 64 bits: the exchange cancels).
+    const int k = out.near.k;
+    bool any = false;
+    for (int j = tid; j < k; j += kRowThreads) {
+        const int token = out.near.tokens[row * k + j];
+        const bool used = token >= 0 && token < in.vocab;
+        mix.token[j] = used ? token : -1;
+        any |= used;
+    }
+    any = __syncthreads_or(any);
+    const float log_model = none ? -INFINITY : any ? out.log_model : 0.f;
+    const float log_near = !any ? -INFINITY : none ? 0.f : out.log_near;
+    if (tid == 0) mix.hit = -INFINITY;
+    double change = 0.0;                                   // of -sum m log m
+    for (int j = tid; j < k; j += kRowThreads) {
+        const int token = mix.token[j];
+        if (token < 0) continue;
+        const float model = log_model + model_logp((float)x[token]);
+        const float mixed = log_add(model, log_near + out.near.values[row * k + j]);
+        mix.logp[j] = mixed;
+        if (model > kLeastPower || model != model) change += (double)expf(model) * (double)model;
+        if (mixed > kLeastPower || mixed != mixed) change -= (double)expf(mixed) * (double)mixed;
+    }
+    change = block_sum<kRowThreads>(change, mix.sums);     // and a barrier behind mix.hit, mix.logp
+    if (out.targets) {
+        const int t = out.targets[row];
+        if (t >= 0)
+            for (int j = tid; j < k; j += kRowThreads)
+                if (mix.token[j] == t) mix.hit = mix.logp[j];
+    }
+    __syncthreads();
+    if (tid == 0) {
+        if (out.entropy) {
+            const double base = none ? 0.0 : exp((double)log_model) * ((double)entropy - (double)log_model);
+            const double h = base + change;
+            out.entropy[row] = h > 0.0 || h != h ? (float)h : 0.f;
+        }
+        if (out.targets) {
+            const bool listed = mix.hit > -INFINITY || mix.hit != mix.hit;
+            out.logprobs[row] = !wanted ? 0.f : listed ? mix.hit : log_model + model_logp((float)x[target]);
+        }
+    }
+    if constexpr (TOP) {
+        // the kept tokens that are not listed, and the listed ones, by their mixed log-probabilities
+        for (int i = tid; i < n_kept; i += kRowThreads) {
+            const int token = key_token(sel->kept[i]);
+            bool listed = false;
+            for (int j = 0; j < k; ++j) listed |= mix.token[j] == token;
+            const float logp = log_model + model_logp(key_value(sel->kept[i]));
+            if (!listed && logp > -INFINITY) sel->found[atomicAdd(&sel->n_found, 1)] = token_key(logp, (uint32_t)token);
+        }
+        for (int j = tid; j < k; j += kRowThreads)
+            if (mix.token[j] >= 0 && mix.logp[j] > -INFINITY)
+                sel->found[atomicAdd(&sel->n_found, 1)] = token_key(mix.logp[j], (uint32_t)mix.token[j]);
+        __syncthreads();
+        const int n = sel->n_found;
+        __syncthreads();
+        const int best = keep_best(*sel, n, 0, out.top);
+        for (int i = tid; i < out.top; i += kRowThreads) {
+            const bool used = i < best;
+            out.top_tokens[row * out.top + i] = used ? key_token(sel->kept[i]) : -1;
+            out.top_logprobs[row * out.top + i] = used ? key_value(sel->kept[i]) : -INFINITY;
+        }
+    }
+}
+
+// The teacher's shares of its listed tokens: P_j of entry j = exp2((value_j - most) scale) / total, total 0 if no entry is used.
+struct Teacher {
+    float most, total;
+};
+__device__ inline bool teacher_uses(const Listed& l, long long row, int j, int vocab) {
+    const int token = l.tokens[row * l.k + j];
+    return token >= 0 && token < vocab && l.values[row * l.k + j] != -INFINITY;
+}
+__device__ inline Teacher teacher_of(const Listed& l, long long row, int vocab, float scale, float* scratch) {
+    float most = -INFINITY;
+    for (int j = threadIdx.x; j < l.k; j += kRowThreads)
+        if (teacher_uses(l, row, j, vocab)) most = fmaxf(most, l.values[row * l.k + j]);
+    most = block_max<kRowThreads>(most, scratch);
+    float total = 0.f;
+    for (int j = threadIdx.x; j < l.k; j += kRowThreads)
+        if (teacher_uses(l, row, j, vocab)) total += exp2_fast((l.values[row * l.k + j] - most) * scale);
+    return Teacher{most, block_sum<kRowThreads>(total, scratch)};
+}
+
+template <class T>
+__device__ inline void finish_distill(const RowsIn& in, const DistillOut& out, long long row, RowSum sum, float* scratch) {
+    const T* x = reinterpret_cast<const T*>(in.data) + row * in.stride;
+    const bool none = sum.s == 0.f;
+    const float log_s = logf(sum.s);
+    const Teacher teacher = teacher_of(out.teacher, row, in.vocab, in.scale, scratch);
+    const float log_total = logf(teacher.total);
+    float loss = 0.f;
+    for (int j = threadIdx.x; j < out.teacher.k; j += kRowThreads) {
+        if (!teacher_uses(out.teacher, row, j, in.vocab)) continue;
+        const float at = (out.teacher.values[row * out.teacher.k + j] - teacher.most) * in.scale;
+        const float share = exp2_fast(at) / teacher.total;
+        if (share == 0.f) continue;
+        const float v = (float)x[out.teacher.tokens[row * out.teacher.k + j]];
+        const float logp = none ? -INFINITY : (v - sum.m) / in.temperature - log_s;
+        loss += share * (__builtin_fmaf(at, kLn2, -log_total) - logp);
+    }
+    loss = block_sum<kRowThreads>(loss, scratch);
+    if (threadIdx.x == 0) {
+        out.loss[row] = loss * in.temperature * in.temperature;
+        write_norms(out.norms, row, sum.m, log_s, none);
+    }
+}
+
+// ---- the pass over the logits
+
+// 16-byte chunks that a thread holds at once
+constexpr int kRowChunks = 4;
+
+template <class T>
+__device__ inline void load_tile(const RowChunks<T>& row, int c0, int end, Chunk<T> (&k)[kRowChunks]) {
+    const int tid = threadIdx.x;
+    if (c0 + kRowChunks * kRowThreads <= end && row.whole(c0) && row.whole(c0 + kRowChunks * kRowThreads - 1)) {
+#pragma unroll
+        for (int i = 0; i < kRowChunks; ++i) k[i].bits = row.base[c0 + i * kRowThreads + tid];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kRowChunks; ++i) {
+        const int c = c0 + i * kRowThreads + tid;
+        if (c < end) k[i] = row.load(c);
+        else {
+            float none[Chunk<T>::VEC];
+#pragma unroll
+            for (int j = 0; j < Chunk<T>::VEC; ++j) none[j] = -INFINITY;
+            k[i].narrow(none);
+        }
+    }
+}
+
+// Adds the chunks to the sums about the thread's own maximum; leaves the maximum of every chunk.
+template <class T, bool ENTROPY>
+__device__ inline void add_tile(Chunk<T> (&k)[kRowChunks], float scale, RowSum& sum, float (&most)[kRowChunks]) {
+    constexpr int VEC = Chunk<T>::VEC;
+    float top = sum.m;
+#pragma unroll
+    for (int i = 0; i < kRowChunks; ++i) {
+        float x[VEC];
+        k[i].widen(x);
+        most[i] = x[0];
+#pragma unroll
+        for (int j = 1; j < VEC; ++j) most[i] = fmaxf(most[i], x[j]);
+        top = fmaxf(top, most[i]);
+    }
+    if (top > sum.m) sum.raise(top, scale);
+    const float ref = sum.m == -INFINITY ? 0.f : sum.m;     // nothing but -inf so far: t = -inf, not a NaN
+#pragma unroll
+    for (int i = 0; i < kRowChunks; ++i) {
+        float x[VEC];
+        k[i].forget_widened();
+        k[i].widen(x);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float t = (x[j] - ref) * scale, e = exp2_fast(t);
+            sum.s += e;
+            if constexpr (ENTROPY) sum.u = __builtin_fmaf(fmaxf(t, kLeastPower), e, sum.u);
+        }
+    }
+}
+
+template <class T>
+__device__ inline uint64_t best_of_tile(const Chunk<T> (&k)[kRowChunks], const float (&most)[kRowChunks], int first_token) {
+    constexpr int VEC = Chunk<T>::VEC;
+    Chunk<T> best = k[0];
+    float top = most[0];
+    int at = 0;
+#pragma unroll
+    for (int i = 1; i < kRowChunks; ++i)
+        if (most[i] > top) { best = k[i]; top = most[i]; at = i; }
+    if (!(top > -INFINITY)) return 0;
+    float x[VEC];
+    best.widen(x);
+    int j0 = 0;
+#pragma unroll
+    for (int j = VEC - 1; j >= 0; --j)
+        if (x[j] == top) j0 = j;
+    return token_key(top, (uint32_t)(first_token + at * kRowThreads * VEC + j0));
+}
+
+enum class RowMode { kScore, kScoreTop, kDistill };
+
+struct RowShared {
+    Partial waves[kRowWaves];
+    float scratch[kRowWaves];
+};
+template <RowMode MODE> struct RowLds { RowShared rows; MixShared mix; };
+template <> struct RowLds<RowMode::kScoreTop> { RowShared rows; MixShared mix; Selection sel; };
+template <> struct RowLds<RowMode::kDistill> { RowShared rows; };
+
+struct RowSplit {
+    int splits, chunks;               // workgroups a row, chunks of each
+    Partial* partials;                // [n][splits]; null with one workgroup a row
+    uint64_t* keys;                   // [n][splits][want], descending, 0 where there are fewer
+};
+
+// the statistics of the workgroup's threads, in all of them
+__device__ inline RowSum block_join(RowSum sum, float scale, RowShared& lds) {
+    sum = wave_join(sum, scale);
+    if ((threadIdx.x & 63) == 0) lds.waves[threadIdx.x >> 6] = Partial{sum.m, sum.s, sum.u, 0.f};
+    __syncthreads();
+    sum = RowSum(lds.waves[0]);
+#pragma unroll
+    for (int w = 1; w < kRowWaves; ++w) sum.join(RowSum(lds.waves[w]), scale);
+    return sum;
+}
+
+template <class T, RowMode MODE, class Out>
+__device__ inline void finish_row(const RowsIn& in, const Out& out, long long row, RowSum sum, int n_kept, RowLds<MODE>& lds) {
+    if constexpr (MODE == RowMode::kScoreTop) finish_score<T, true>(in, out, row, sum, n_kept, &lds.sel, lds.mix);
+    else if constexpr (MODE == RowMode::kScore) finish_score<T, false>(in, out, row, sum, 0, nullptr, lds.mix);
+    else finish_distill<T>(in, out, row, sum, lds.rows.scratch);
+}
+
+// One workgroup: the chunks [split * chunks, ...) of a row.
+template <class T, RowMode MODE, class Out>
+__global__ __launch_bounds__(kRowThreads, 4) void row_statistics_kernel(RowsIn in, RowSplit split, Out out) {
+    constexpr int VEC = Chunk<T>::VEC;
+    constexpr bool TOP = MODE == RowMode::kScoreTop, ENTROPY = MODE != RowMode::kDistill;
+    __shared__ RowLds<MODE> lds;
+    const long long r = blockIdx.x / (unsigned)split.splits;
+    const int part = blockIdx.x % (unsigned)split.splits;
+    const RowChunks<T> row(in.data, r, in.stride, in.vocab);
+    const int begin = part * split.chunks;
+    const int end = min(begin + split.chunks, row.count());
+    RowSum sum;
+    uint64_t bound = 0;
+    int n_kept = 0, want = 0;
+    if constexpr (TOP) {
+        want = out.want;
+        if (threadIdx.x == 0) lds.sel.n_found = 0;
+        __syncthreads();
+    }
+    Chunk<T> now[kRowChunks], next[kRowChunks];
+    if (begin < end) load_tile(row, begin, end, now);
+    for (int c0 = begin; c0 < end; c0 += kRowChunks * kRowThreads) {
+        const int c1 = c0 + kRowChunks * kRowThreads;
+        if (c1 < end) load_tile(row, c1, end, next);
+        float most[kRowChunks];
+        add_tile<T, ENTROPY>(now, in.scale, sum, most);
+        if constexpr (TOP) {
+            const int first = (c0 + (int)threadIdx.x) * VEC - row.lead;
+            if (n_kept < want) bound = bound_of_best(lds.sel, best_of_tile(now, most, first), want);
+            n_kept = take_candidates(lds.sel, bound, n_kept, want, [&](uint64_t b, auto push) {
+                const float least = b ? key_value(b) : -INFINITY;
+                int token0 = first;
+                asm volatile("" : "+v"(token0));           // tokens are formed where they are needed, not kept in registers
+#pragma unroll
+                for (int i = 0; i < kRowChunks; ++i) {
+                    if (!(most[i] >= least)) continue;
+                    float x[VEC];
+                    now[i].forget_widened();
+                    now[i].widen(x);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j)
+                        if (x[j] >= least && x[j] > -INFINITY) {
+                            const uint64_t key = token_key(x[j], (uint32_t)(token0 + i * kRowThreads * VEC + j));
+                            if (key >= b) push(key);
+                        }
+                }
+            });
+        }
+#pragma unroll
+        for (int i = 0; i < kRowChunks; ++i) now[i] = next[i];
+    }
+    sum = block_join(sum, in.scale, lds.rows);
+    if (split.splits == 1) {
+        __syncthreads();
+        finish_row<T, MODE>(in, out, r, sum, n_kept, lds);
+        return;
+    }
+    const long long at = r * split.splits + part;
+    if (threadIdx.x == 0) split.partials[at] = Partial{sum.m, sum.s, sum.u, 0.f};
+    if constexpr (TOP)
+        for (int i = threadIdx.x; i < want; i += kRowThreads) split.keys[at * want + i] = i < n_kept ? lds.sel.kept[i] : 0;
+}
+
+// One workgroup a row: joins what the row's workgroups left.
+template <class T, RowMode MODE, class Out>
+__global__ __launch_bounds__(kRowThreads) void row_join_kernel(RowsIn in, RowSplit split, Out out) {
+    __shared__ RowLds<MODE> lds;
+    const long long r = blockIdx.x;
+    RowSum sum;
+    if ((int)threadIdx.x < split.splits) sum = RowSum(split.partials[r * split.splits + threadIdx.x]);
+    sum = block_join(sum, in.scale, lds.rows);
+    int n_kept = 0;
+    if constexpr (MODE == RowMode::kScoreTop) {
+        const int want = out.want;
+        const uint64_t* keys = split.keys + r * split.splits * (long long)want;
+        // every workgroup's q-th largest key bounds q keys from below; together splits * q >= want
+        const int q = (want + split.splits - 1) / split.splits;
+        uint64_t low = ~(uint64_t)0, high = 0;
+        for (int p = 0; p < split.splits; ++p) {
+            const uint64_t a = keys[(long long)p * want + q - 1], b = keys[(long long)p * want + want - 1];
+            low = a < low ? a : low;
+            high = b > high ? b : high;
+        }
+        uint64_t bound = low > high ? low : high;
+        if (threadIdx.x == 0) lds.sel.n_found = 0;
+        __syncthreads();
+        n_kept = take_candidates(lds.sel, bound, 0, want, [&](uint64_t b, auto push) {
+            for (int i = threadIdx.x; i < split.splits * want; i += kRowThreads) {
+                const uint64_t key = keys[i];
+                if (key >= b && key) push(key);
+            }
+        });
+    }
+    __syncthreads();
+    finish_row<T, MODE>(in, out, r, sum, n_kept, lds);
+}
+
+// ---- gradients
+
+struct GradIn {
+    const float* norms;               // [n][2]
+    void* grad;
+    long long grad_stride;
+    int chunks;                       // of a workgroup
+    int splits;
+};
+struct PolicyGrad {
+    const int32_t* targets;
+    const float *entropy, *by_logprob, *by_entropy;
+};
+struct DistillGrad {
+    Listed teacher;
+    const float* row_grads;
+};
+
+struct GradShared {
+    float scratch[kRowWaves];
+    int token[IVFPQ_MAX_LISTED];
+    float share[IVFPQ_MAX_LISTED];
+    float x[IVFPQ_MAX_LISTED];
+};
+
+// grad_v = p_v (a + b t_v), t_v = log2 p_v, plus a term at a few listed tokens; a row without a distribution has zeros.
+// One workgroup: the chunks [split * chunks, ...) of a row.  The listed tokens' logits are read before anything is
+// written (the gradient may lie over the logits) and their elements written again after a barrier.
+template <class T, bool BY_ENTROPY, class How>
+__global__ __launch_bounds__(kRowThreads) void row_gradient_kernel(RowsIn in, GradIn g, How how) {
+    constexpr int VEC = Chunk<T>::VEC;
+    constexpr bool POLICY = std::is_same<How, PolicyGrad>::value;
+    __shared__ GradShared lds;
+    const int tid = threadIdx.x;
+    const long long r = blockIdx.x / (unsigned)g.splits;
+    const int part = blockIdx.x % (unsigned)g.splits;
+    const RowChunks<T> row(in.data, r, in.stride, in.vocab), to(g.grad, r, g.grad_stride, in.vocab);
+    T* grad = const_cast<T*>(to.row);
+    const int begin = part * g.chunks;
+    const int end = min(begin + g.chunks, row.count());
+    const int token0 = max(begin * VEC - row.lead, 0), token1 = min(end * VEC - row.lead, in.vocab);    // the workgroup's
+    const float m = g.norms[2 * r], log2_s = g.norms[2 * r + 1] * kLog2E;
+    const bool none = m == -INFINITY;
+    float a = 0.f, b = 0.f;
+    int k = 0;
+    if constexpr (POLICY) {
+        const float by_logprob = how.by_logprob ? how.by_logprob[r] : 0.f;
+        const int target = how.targets ? how.targets[r] : -1;
+        const bool wanted = target >= 0 && target < in.vocab;
+        const float gl = wanted ? by_logprob / in.temperature : 0.f;
+        a = -gl;
+        if constexpr (BY_ENTROPY) {
+            const float gh = how.by_entropy[r] / in.temperature;
+            a -= gh * how.entropy[r];
+            b = -gh * kLn2;
+        }
+        k = wanted && how.by_logprob ? 1 : 0;
+        if (tid == 0 && k) {
+            lds.token[0] = target;
+            lds.share[0] = gl;
+            lds.x[0] = target >= token0 && target < token1 ? row.value(target) : 0.f;
+        }
+    } else {
+        const Teacher teacher = teacher_of(how.teacher, r, in.vocab, in.scale, lds.scratch);
+        const float w = in.temperature * (how.row_grads ? how.row_grads[r] : 1.f);
+        k = how.teacher.k;
+        for (int j = tid; j < k; j += kRowThreads) {
+            const bool used = teacher_uses(how.teacher, r, j, in.vocab);
+            const int token = used ? how.teacher.tokens[r * k + j] : -1;
+            lds.token[j] = token;
+            lds.share[j] = used ? -w * exp2_fast((how.teacher.values[r * k + j] - teacher.most) * in.scale) / teacher.total : 0.f;
+            lds.x[j] = used && token >= token0 && token < token1 ? row.value(token) : 0.f;
+        }
+        a = teacher.total == 0.f ? 0.f : w;                // a NaN among the values stays one
+    }
+    __syncthreads();
+    auto dense = [&](float x) {
+        const float t = __builtin_fmaf(x - m, in.scale, -log2_s);
+        const float p = exp2_fast(t);
+        if constexpr (BY_ENTROPY) return p * __builtin_fmaf(b, fmaxf(t, kLeastPower), a);
+        else return p * a;
+    };
+    const bool alike = to.lead == row.lead;                // chunks of both lie alike
+    for (int c = begin + tid; c < end; c += kRowThreads) {
+        float x[VEC];
+        row.load(c).widen(x);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[j] = none ? 0.f : dense(x[j]);
+        if (alike && row.whole(c)) {
+            Chunk<T> y;
+            y.narrow(x);
+            const_cast<uint4*>(to.base)[c] = y.bits;
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const int v = c * VEC + j - row.lead;
+                if (v >= 0 && v < in.vocab) grad[v] = (T)x[j];
+            }
+        }
+    }
+    if (none) return;
+    __syncthreads();
+    for (int j = tid; j < k; j += kRowThreads) {
+        const int token = lds.token[j];
+        if (token < token0 || token >= token1) continue;
+        float share = lds.share[j];
+        bool first = true;
+        if constexpr (!POLICY)                             // entries of one token add up, in their order, at the first of them
+            for (int i = 0; i < k; ++i)
+                if (i != j && lds.token[i] == token) {
+                    first &= i > j;
+                    share += lds.share[i];
+                }
+        if (first) grad[token] = (T)(dense(lds.x[j]) + share);
+    }
+}
+
+// ---- launches
+
+constexpr int64_t kMostRows = 1 << 23;                      // a launch has fewer than 2^32 threads
+constexpr float kLeastTemperature = 1e-6f, kMostTemperature = 1e6f;       // T^2 and log2(e) / T stay moderate
+
+// How a row is dealt to workgroups: enough of them to fill the GPU, at least a chunk for every thread, at most kMostSplits.
+RowSplit split_rows(int64_t n, int32_t vocab, int vec, int most_splits) {
+    constexpr int64_t kFill = 1024;                        // four workgroups on each of 256 CUs
+    const int64_t chunks = ((int64_t)vocab + vec - 1) / vec + 1;      // of a row at the worst alignment
+    const int64_t useful = (chunks + kRowThreads - 1) / kRowThreads;
+    int64_t splits = std::min<int64_t>({(kFill + n - 1) / n, useful, most_splits});
+    RowSplit s{};
+    s.chunks = (int)((chunks + splits - 1) / splits);
+    s.chunks = (s.chunks + kRowThreads - 1) / kRowThreads * kRowThreads;
+    s.splits = (int)((chunks + s.chunks - 1) / s.chunks);
+    return s;
+}
+
+int check_rows(const char* what, const void* data, int32_t dtype, int64_t n, int32_t vocab, int64_t stride, float temperature) {
+    if (!known_dtype(dtype)) return fail(IVFPQ_EINVAL, "%s: unknown dtype %d", what, dtype);
+    if (n < 0 || vocab < 1) return fail(IVFPQ_EINVAL, "%s: bad shape (n=%lld vocab=%d)", what, (long long)n, vocab);
+    if (vocab > (1 << 30)) return fail(IVFPQ_EUNSUPPORTED, "%s: vocab=%d (limit 2^30)", what, vocab);
+    if (n > kMostRows) return fail(IVFPQ_EUNSUPPORTED, "%s: n=%lld (limit 2^23 rows per call)", what, (long long)n);
+    if (n > 1 && stride < vocab) return fail(IVFPQ_EINVAL, "%s: row stride %lld below vocab=%d", what, (long long)stride, vocab);
+    if (!(temperature >= kLeastTemperature && temperature <= kMostTemperature))
+        return fail(IVFPQ_EINVAL, "%s: temperature outside [%g, %g]", what, (double)kLeastTemperature, (double)kMostTemperature);
+    if (n > 0 && !data) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
+    if ((uintptr_t)data % value_bytes(dtype)) return fail(IVFPQ_EINVAL, "%s: logits are not aligned to their type", what);
+    return IVFPQ_OK;
+}
+
+int check_grad(const char* what, const void* logits, int64_t stride, const void* grad, int32_t dtype, int64_t n, int32_t vocab, int64_t grad_stride) {
+    if (n > 0 && !grad) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
+    if (n > 1 && grad_stride < vocab) return fail(IVFPQ_EINVAL, "%s: gradient stride %lld below vocab=%d", what, (long long)grad_stride, vocab);
+    if ((uintptr_t)grad % value_bytes(dtype)) return fail(IVFPQ_EINVAL, "%s: the gradient is not aligned to its type", what);
+    if (n > 0) {
+        const size_t vb = value_bytes(dtype);
+        const uintptr_t a = (uintptr_t)logits, b = (uintptr_t)grad;
+        const uintptr_t a1 = a + ((size_t)(n - 1) * stride + vocab) * vb, b1 = b + ((size_t)(n - 1) * grad_stride + vocab) * vb;
+        const size_t width = (size_t)vocab * vb, pitch = (size_t)stride * vb;
+        const size_t apart = n > 1 ? (a < b ? b - a : a - b) % pitch : 0;         // columns of one wider matrix
+        const bool beside = n > 1 && stride == grad_stride && apart >= width && apart <= pitch - width;
+        if (a < b1 && b < a1 && !beside && !(a == b && (n == 1 || stride == grad_stride)))
+            return fail(IVFPQ_EINVAL, "%s: the gradient overlaps the logits without lying over them", what);
+    }
+    return IVFPQ_OK;
+}
+
+int check_listed(const char* what, const int32_t* tokens, const float* values, int64_t n, int32_t k) {
+    if (k < 1 || k > IVFPQ_MAX_LISTED) return fail(IVFPQ_EINVAL, "%s: k=%d outside [1, %d]", what, k, (int)IVFPQ_MAX_LISTED);
+    if (n > 0 && (!tokens || !values)) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
+    return IVFPQ_OK;
+}
+
+int check_workspace(const char* what, const void* ws, size_t bytes, size_t need) {
+    if (need == 0) return IVFPQ_OK;
+    if (!ws) return fail(IVFPQ_EINVAL, "%s: null workspace", what);
+    if ((uintptr_t)ws % kAlign) return fail(IVFPQ_EINVAL, "%s: workspace not aligned to %zu bytes", what, kAlign);
+    if (bytes < need) return fail(IVFPQ_ENOSPACE, "%s: workspace %zu bytes, need %zu", what, bytes, need);
+    return IVFPQ_OK;
+}
+
+RowsIn rows_in(const void* data, int64_t stride, int32_t vocab, float temperature) {
+    return RowsIn{data, stride, vocab, temperature, (float)(1.4426950408889634 / (double)temperature)};
+}
+
+// scratch of the split rows of `n`: partial sums, then keys
+size_t split_bytes(int64_t n, const RowSplit& s, int want) {
+    if (s.splits == 1) return 0;
+    return align_up((size_t)n * s.splits * sizeof(Partial)) + align_up((size_t)n * s.splits * want * sizeof(uint64_t));
+}
+
+// the largest over the value types
+size_t row_workspace(int64_t n, int32_t vocab, int want) {
+    if (n < 1 || vocab < 1 || vocab > (1 << 30) || n > kMostRows) return 0;
+    return std::max(split_bytes(n, split_rows(n, vocab, 4, kMostSplits), want), split_bytes(n, split_rows(n, vocab, 8, kMostSplits), want));
+}
+
+template <class T, RowMode MODE, class Out>
+int launch_rows(int64_t n, const RowsIn& in, const Out& out, int want, void* ws, hipStream_t stream) {
+    RowSplit s = split_rows(n, in.vocab, Chunk<T>::VEC, kMostSplits);
+    if (s.splits > 1) {
+        s.partials = (Partial*)ws;
+        s.keys = (uint64_t*)((char*)ws + align_up((size_t)n * s.splits * sizeof(Partial)));
+    }
+    (void)want;
+    hipLaunchKernelGGL((row_statistics_kernel<T, MODE, Out>), dim3((unsigned)(n * s.splits)), dim3(kRowThreads), 0, stream, in, s, out);
+    HIP_TRY(hipGetLastError());
+    if (s.splits > 1) {
+        hipLaunchKernelGGL((row_join_kernel<T, MODE, Out>), dim3((unsigned)n), dim3(kRowThreads), 0, stream, in, s, out);
+        HIP_TRY(hipGetLastError());
+    }
+    return IVFPQ_OK;
+}
+
+template <class T, bool BY_ENTROPY, class How>
+int launch_gradient(int64_t n, const RowsIn& in, GradIn g, const How& how, hipStream_t stream) {
+    const RowSplit s = split_rows(n, in.vocab, Chunk<T>::VEC, kMostSplits);
+    g.splits = s.splits;
+    g.chunks = s.chunks;
+    hipLaunchKernelGGL((row_gradient_kernel<T, BY_ENTROPY, How>), dim3((unsigned)(n * s.splits)), dim3(kRowThreads), 0, stream, in, g, how);
+    HIP_TRY(hipGetLastError());
+    return IVFPQ_OK;
+}
+
+int token_logprobs(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab, int64_t row_stride, const int32_t* d_targets,
+                   float temperature, int32_t top, const int32_t* d_neighbour_tokens, const float* d_neighbour_logprobs,
+                   int32_t n_neighbours, float weight, float* d_logprobs, float* d_entropy, float* d_norms, int32_t* d_top_tokens,
+                   float* d_top_logprobs, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    const char* what = "ivfpq_token_logprobs";
+    if (int s = check_rows(what, d_logits, dtype, n, vocab, row_stride, temperature)) return s;
+    if (top < 0 || top > IVFPQ_MAX_TOP) return fail(IVFPQ_EINVAL, "%s: top=%d outside [0, %d]", what, top, (int)IVFPQ_MAX_TOP);
+    if (n_neighbours < 0 || n_neighbours > IVFPQ_MAX_LISTED)
+        return fail(IVFPQ_EINVAL, "%s: n_neighbours=%d outside [0, %d]", what, n_neighbours, (int)IVFPQ_MAX_LISTED);
+    if (top && n_neighbours && top + n_neighbours > IVFPQ_MAX_MIXED)
+        return fail(IVFPQ_EUNSUPPORTED, "%s: %d alternatives and %d neighbours, together over %d", what, top, n_neighbours, (int)IVFPQ_MAX_MIXED);
+    if (n_neighbours && !(weight > 0.f && weight < 1.f)) return fail(IVFPQ_EINVAL, "%s: weight must be above 0 and below 1", what);
+    if (n == 0) return IVFPQ_OK;
+    if (n_neighbours && (!d_neighbour_tokens || !d_neighbour_logprobs)) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
+    if ((d_targets == nullptr) != (d_logprobs == nullptr)) return fail(IVFPQ_EINVAL, "%s: targets and logprobs go together", what);
+    if (top && (!d_top_tokens || !d_top_logprobs)) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
+    const int want = top ? top + n_neighbours : 0;
+    if (int s = check_workspace(what, d_workspace, workspace_bytes, row_workspace(n, vocab, want))) return s;
+    const RowsIn in = rows_in(d_logits, row_stride, vocab, temperature);
+    const ScoreOut out{d_targets, Listed{d_neighbour_tokens, d_neighbour_logprobs, n_neighbours},
+                       n_neighbours ? (float)std::log1p(-(double)weight) : 0.f, n_neighbours ? (float)std::log((double)weight) : 0.f, top, want,
+                       d_logprobs, d_entropy, d_norms, d_top_tokens, d_top_logprobs};
+    return with_value_type(dtype, [&](auto v) {
+        using T = decltype(v);
+        if (top) return launch_rows<T, RowMode::kScoreTop>(n, in, out, want, d_workspace, (hipStream_t)hip_stream);
+        return launch_rows<T, RowMode::kScore>(n, in, out, want, d_workspace, (hipStream_t)hip_stream);
+    });
+}
+
+int distill_forward(const char* what, const RowsIn& in, int32_t dtype, int64_t n, const Listed& teacher, float* d_loss, float* d_norms,
+                    void* d_workspace, hipStream_t stream) {
+    const DistillOut out{teacher, d_loss, d_norms};
+    return with_value_type(dtype, [&](auto v) {
+        return launch_rows<decltype(v), RowMode::kDistill>(n, in, out, 0, d_workspace, stream);
+    });
+}
+
+int distill_gradient(const RowsIn& in, int32_t dtype, int64_t n, const Listed& teacher, const float* d_row_grads, const float* d_norms,
+                     void* d_grad, int64_t grad_stride, hipStream_t stream) {
+    GradIn g{};
+    g.norms = d_norms;
+    g.grad = d_grad;
+    g.grad_stride = grad_stride;
+    const DistillGrad how{teacher, d_row_grads};
+    return with_value_type(dtype, [&](auto v) { return launch_gradient<decltype(v), false>(n, in, g, how, stream); });
+}
+
+size_t distill_scratch(int64_t n, int32_t vocab) {
+    if (n < 1 || n > kMostRows) return 0;
+    return align_up((size_t)n * 2 * sizeof(float)) + row_workspace(n, vocab, 0);      // norms of a step, then the split rows
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ivfpq_token_logprobs_workspace_bytes(int64_t n, int32_t vocab, int32_t top, int32_t n_neighbours) {
+    if (top < 0 || top > IVFPQ_MAX_TOP || n_neighbours < 0 || n_neighbours > IVFPQ_MAX_LISTED) return 0;
+    return row_workspace(n, vocab, top ? std::min<int>(top + n_neighbours, IVFPQ_MAX_MIXED) : 0);
+}
+
+int ivfpq_token_logprobs(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab, int64_t row_stride, const int32_t* d_targets,
+                         float temperature, int32_t top, const int32_t* d_neighbour_tokens, const float* d_neighbour_logprobs,
+                         int32_t n_neighbours, float weight, float* d_logprobs, float* d_entropy, float* d_norms,
+                         int32_t* d_top_tokens, float* d_top_logprobs, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    return guarded("ivfpq_token_logprobs", [&] {
+        return token_logprobs(d_logits, dtype, n, vocab, row_stride, d_targets, temperature, top, d_neighbour_tokens, d_neighbour_logprobs,
+                              n_neighbours, weight, d_logprobs, d_entropy, d_norms, d_top_tokens, d_top_logprobs, d_workspace,
+                              workspace_bytes, hip_stream);
+    });
+}
+
+int ivfpq_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab, int64_t row_stride,
+                                  const int32_t* d_targets, float temperature, const float* d_norms, const float* d_entropy,
+                                  const float* d_grad_logprobs, const float* d_grad_entropy, void* d_grad, int64_t grad_stride,
+                                  void* hip_stream) {
+    return guarded("ivfpq_token_logprobs_backward", [&] {
+        const char* what = "ivfpq_token_logprobs_backward";
+        if (int s = check_rows(what, d_logits, dtype, n, vocab, row_stride, temperature)) return s;
+        if (int s = check_grad(what, d_logits, row_stride, d_grad, dtype, n, vocab, grad_stride)) return s;
+        if (n == 0) return (int)IVFPQ_OK;
+        if (!d_norms) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
+        if (!d_grad_logprobs && !d_grad_entropy) return fail(IVFPQ_EINVAL, "%s: neither gradient is given", what);
+        if (d_grad_logprobs && !d_targets) return fail(IVFPQ_EINVAL, "%s: gradients of log-probabilities without targets", what);
+        if (d_grad_entropy && !d_entropy) return fail(IVFPQ_EINVAL, "%s: gradients of entropies without entropies", what);
+        const RowsIn in = rows_in(d_logits, row_stride, vocab, temperature);
+        GradIn g{};
+        g.norms = d_norms;
+        g.grad = d_grad;
+        g.grad_stride = grad_stride;
+        const PolicyGrad how{d_targets, d_entropy, d_grad_logprobs, d_grad_entropy};
+        return with_value_type(dtype, [&](auto v) {
+            using T = decltype(v);
+            if (d_grad_entropy) return launch_gradient<T, true>(n, in, g, how, (hipStream_t)hip_stream);
+            return launch_gradient<T, false>(n, in, g, how, (hipStream_t)hip_stream);
+        });
+    });
+}
+
+size_t ivfpq_distill_topk_workspace_bytes(int64_t n, int32_t vocab) { return distill_scratch(n, vocab); }
+
+int ivfpq_distill_topk(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab, int64_t row_stride, const int32_t* d_teacher_tokens,
+                       const float* d_teacher_logits, int32_t k, float temperature, float* d_loss, float* d_norms, void* d_workspace,
+                       size_t workspace_bytes, void* hip_stream) {
+    return guarded("ivfpq_distill_topk", [&] {
+        const char* what = "ivfpq_distill_topk";
+        if (int s = check_rows(what, d_logits, dtype, n, vocab, row_stride, temperature)) return s;
+        if (int s = check_listed(what, d_teacher_tokens, d_teacher_logits, n, k)) return s;
+        if (n == 0) return (int)IVFPQ_OK;
+        if (!d_loss || !d_norms) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
+        if (int s = check_workspace(what, d_workspace, workspace_bytes, distill_scratch(n, vocab))) return s;
+        void* split = (char*)d_workspace + align_up((size_t)n * 2 * sizeof(float));
+        return distill_forward(what, rows_in(d_logits, row_stride, vocab, temperature), dtype, n, Listed{d_teacher_tokens, d_teacher_logits, k},
+                               d_loss, d_norms, split, (hipStream_t)hip_stream);
+    });
+}
+
+int ivfpq_distill_topk_backward(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab, int64_t row_stride, const float* d_norms,
+                                const int32_t* d_teacher_tokens, const float* d_teacher_logits, int32_t k, float temperature,
+                                const float* d_row_grads, void* d_grad, int64_t grad_stride, void* hip_stream) {
+    return guarded("ivfpq_distill_topk_backward", [&] {
+        const char* what = "ivfpq_distill_topk_backward";
+        if (int s = check_rows(what, d_logits, dtype, n, vocab, row_stride, temperature)) return s;
+        if (int s = check_listed(what, d_teacher_tokens, d_teacher_logits, n, k)) return s;
+        if (int s = check_grad(what, d_logits, row_stride, d_grad, dtype, n, vocab, grad_stride)) return s;
+        if (n == 0) return (int)IVFPQ_OK;
+        if (!d_norms) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
+        return distill_gradient(rows_in(d_logits, row_stride, vocab, temperature), dtype, n, Listed{d_teacher_tokens, d_teacher_logits, k},
+                                d_row_grads, d_norms, d_grad, grad_stride, (hipStream_t)hip_stream);
+    });
+}
+
+int ivfpq_distill_topk_step(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab, int64_t row_stride,
+                            const int32_t* d_teacher_tokens, const float* d_teacher_logits, int32_t k, float temperature,
+                            const float* d_row_grads, float* d_loss, void* d_grad, int64_t grad_stride, void* d_workspace,
+                            size_t workspace_bytes, void* hip_stream) {
+    return guarded("ivfpq_distill_topk_step", [&] {
+        const char* what = "ivfpq_distill_topk_step";
+        if (int s = check_rows(what, d_logits, dtype, n, vocab, row_stride, temperature)) return s;
+        if (int s = check_listed(what, d_teacher_tokens, d_teacher_logits, n, k)) return s;
+        if (int s = check_grad(what, d_logits, row_stride, d_grad, dtype, n, vocab, grad_stride)) return s;
+        if (n == 0) return (int)IVFPQ_OK;
+        if (!d_loss) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
+        if (int s = check_workspace(what, d_workspace, workspace_bytes, distill_scratch(n, vocab))) return s;
+        float* norms = (float*)d_workspace;
+        void* split = (char*)d_workspace + align_up((size_t)n * 2 * sizeof(float));
+        const RowsIn in = rows_in(d_logits, row_stride, vocab, temperature);
+        const Listed teacher{d_teacher_tokens, d_teacher_logits, k};
+        const hipStream_t stream = (hipStream_t)hip_stream;
+        if (int s = distill_forward(what, in, dtype, n, teacher, d_loss, norms, split, stream)) return s;
+        return distill_gradient(in, dtype, n, teacher, d_row_grads, norms, d_grad, grad_stride, stream);
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,150 @@
+// Search results as a distribution over tokens: what ivfpq_neighbour_tokens does.
+//
+// With t_j = (d_min - d_j) log2(e) / T the weight of neighbour j is 2^t_j; the neighbours that share a token add up at the
+// first of them.  A query's neighbours are in the LDS and each is compared with all the others (k^2 comparisons a query).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "ivfpq_hip_util.hpp"
+#include "ivfpq_values.hpp"
+
+using namespace ivfpq;
+
+namespace {
+
+struct NeighboursIn {
+    const long long* ids;             // [nq][k]
+    const float* dists;
+    const int* id_tokens;             // [n_ids]
+    long long n_ids;
+    float scale;                      // log2(e) / T
+    int k;
+};
+
+// One workgroup a query; K: room for neighbours.
+template <int THREADS, int K>
+__global__ __launch_bounds__(THREADS) void neighbour_tokens_kernel(NeighboursIn in, int* __restrict__ tokens, float* __restrict__ logprobs) {
+    constexpr int EACH = K / THREADS, WAVES = THREADS / 64;
+    __shared__ int token[K];
+    __shared__ float weight[K], power[K];
+    __shared__ float scratch[WAVES];
+    __shared__ int firsts[EACH * WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = in.k;
+    const long long q = blockIdx.x;
+    int mine[EACH];
+    float dist[EACH];
+    float nearest = INFINITY;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int j = i * THREADS + tid;
+        mine[i] = -1;
+        dist[i] = INFINITY;
+        if (j < k) {
+            const long long id = in.ids[q * k + j];
+            const float d = in.dists[q * k + j];
+            if (id >= 0 && id < in.n_ids && fabsf(d) < INFINITY) {
+                mine[i] = in.id_tokens[id];
+                if (mine[i] >= 0) dist[i] = d;
+            }
+        }
+        nearest = fminf(nearest, dist[i]);
+    }
+    nearest = -block_max<THREADS>(-nearest, scratch);
+    float total = 0.f;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int j = i * THREADS + tid;
+        if (j >= k) continue;
+        const float t = mine[i] >= 0 ? (nearest - dist[i]) * in.scale : -INFINITY;
+        const float w = exp2_fast(t);
+        token[j] = mine[i];
+        power[j] = t;
+        weight[j] = w;
+        total += w;
+    }
+    const float log_total = logf(block_sum<THREADS>(total, scratch));
+
+    float logp[EACH];
+    bool first[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int j = i * THREADS + tid;
+        first[i] = false;
+        if (j >= k || mine[i] < 0) continue;
+        bool lead = true;
+        float sum = 0.f;
+        for (int o = 0; o < k; ++o) {
+            const bool same = token[o] == mine[i];
+            sum += same ? weight[o] : 0.f;
+            lead &= !(same && o < j);
+        }
+        first[i] = lead;
+        if (!lead) continue;
+        float most = 0.f;
+        if (sum < 1e-30f) {                                // far neighbours only: about the nearest of them
+            most = -INFINITY;
+            for (int o = 0; o < k; ++o)
+                if (token[o] == mine[i]) most = fmaxf(most, power[o]);
+            sum = 0.f;
+            for (int o = 0; o < k; ++o)
+                if (token[o] == mine[i]) sum += exp2_fast(power[o] - most);
+        }
+        logp[i] = most == -INFINITY ? most : most * kLn2 + logf(sum) - log_total;       // -inf: over 10^38 temperatures away
+    }
+    // places: the distinct tokens before this one
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const uint64_t mask = __ballot(first[i]);
+        if (lane == 0) firsts[i * WAVES + wave] = __popcll(mask);
+    }
+    __syncthreads();
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            if (w == wave) {
+                const uint64_t mask = __ballot(first[i]);
+                if (first[i]) {
+                    const int at = before + __popcll(mask & (((uint64_t)1 << lane) - 1));
+                    tokens[q * k + at] = mine[i];
+                    logprobs[q * k + at] = logp[i];
+                }
+            }
+            before += firsts[i * WAVES + w];
+        }
+    for (int j = before + tid; j < k; j += THREADS) {
+        tokens[q * k + j] = -1;
+        logprobs[q * k + j] = -INFINITY;
+    }
+}
+
+}  // namespace
+
+extern "C" int ivfpq_neighbour_tokens(const int64_t* d_ids, const float* d_dists, int64_t nq, int32_t k, const int32_t* d_id_tokens,
+                                      int64_t n_ids, float temperature, int32_t* d_tokens, float* d_logprobs, void* hip_stream) {
+    return guarded("ivfpq_neighbour_tokens", [&] {
+        const char* what = "ivfpq_neighbour_tokens";
+        if (nq < 0 || n_ids < 0) return fail(IVFPQ_EINVAL, "%s: bad shape", what);
+        if (k < 1 || k > IVFPQ_MAX_LISTED) return fail(IVFPQ_EINVAL, "%s: k=%d outside [1, %d]", what, k, (int)IVFPQ_MAX_LISTED);
+        if (!(temperature >= 1e-30f && temperature <= 1e30f)) return fail(IVFPQ_EINVAL, "%s: temperature outside [1e-30, 1e30]", what);
+        if (nq == 0) return (int)IVFPQ_OK;
+        if (!d_ids || !d_dists || !d_tokens || !d_logprobs || (n_ids > 0 && !d_id_tokens)) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
+        const hipStream_t stream = (hipStream_t)hip_stream;
+        constexpr int64_t kPiece = 1 << 22;                // a launch has fewer than 2^32 threads
+        for (int64_t at = 0; at < nq; at += kPiece) {
+            const NeighboursIn in{(const long long*)d_ids + at * k, d_dists + at * k, d_id_tokens, (long long)n_ids,
+                                  (float)(1.4426950408889634 / (double)temperature), k};
+            int* tokens = d_tokens + at * k;
+            float* logprobs = d_logprobs + at * k;
+            const dim3 grid((unsigned)std::min(kPiece, nq - at));
+            if (k <= 64) hipLaunchKernelGGL((neighbour_tokens_kernel<64, 64>), grid, dim3(64), 0, stream, in, tokens, logprobs);
+            else if (k <= 128) hipLaunchKernelGGL((neighbour_tokens_kernel<64, 128>), grid, dim3(64), 0, stream, in, tokens, logprobs);
+            else if (k <= 256) hipLaunchKernelGGL((neighbour_tokens_kernel<256, 256>), grid, dim3(256), 0, stream, in, tokens, logprobs);
+            else hipLaunchKernelGGL((neighbour_tokens_kernel<256, 1024>), grid, dim3(256), 0, stream, in, tokens, logprobs);
+            HIP_TRY(hipGetLastError());
+        }
+        return (int)IVFPQ_OK;
+    });
+}

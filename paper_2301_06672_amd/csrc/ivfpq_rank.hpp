@@ -1,4 +1,4 @@
-// Device code shared by the search kernels and the index builder: order-preserving float keys and the MFMA ranking
+// Device code shared by the search kernels and the index builder: the MFMA ranking
 // GEMMs |c|^2 - 2 x.c (fp32, and bf16 on split operands) with their epilogue (all keys, or per-strip summaries) and the bound of their error.
 // Included by .hip translation units only; everything has internal linkage.
 #pragma once
@@ -7,6 +7,7 @@
 
 #include <type_traits>
 
+#include "ivfpq_float_key.hpp"
 #include "ivfpq_hip_util.hpp"
 #include "ivfpq_probe_rules.hpp"
 
@@ -29,14 +30,6 @@ using ivfpq::coarse_use_strips;
 // ================================================================================================
 constexpr int CK = 16;   // components per LDS slice
 typedef float floatx16 __attribute__((ext_vector_type(16)));
-
-__device__ inline uint32_t ordered_key(float f) {          // monotone map float -> uint32
-    const uint32_t b = __float_as_uint(f);
-    return b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
-}
-__device__ inline float ordered_key_value(uint32_t key) {
-    return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu));
-}
 
 // The three smallest, over the 32 lanes of a half-wave, of 16 values per lane (each lane brings its own
 // three smallest, lo1 <= lo2 <= lo3), folded so that every exchange carries only what the receiver keeps: the lane
