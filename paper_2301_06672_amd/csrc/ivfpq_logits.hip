@@ -5,7 +5,8 @@
 //   S = sum 2^t,  U = sum t 2^t,   log p_v = ln2 (t_v - log2 S),   entropy = ln2 (log2 S - U / S).
 // Both terms of the entropy are non-negative (t <= 0), so nothing cancels.  Partial results (m, s, u) about an own maximum m
 // combine by shifting: s 2^d, (u + d s) 2^d, d = (m - M) log2(e) / T.  One pass over the logits is enough, and a row can be
-// split between workgroups.  x - M is formed before the scale, which keeps masks of the type's lowest value finite.
+// split between workgroups.  x - M is formed before the scale: a fused x scale - M scale would save one of eleven
+// operations an element, but leaves fp32 where a row has nothing but masks of the type's lowest value.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -109,13 +110,17 @@ __device__ inline int keep_best(Selection& sel, int n, int n_kept, int want) {
     const int keep = total < want ? total : want;
     if (total <= 2 * kRowThreads) {
         __syncthreads();
-        for (int i = tid; i < total; i += kRowThreads) {
+        // `share` neighbouring lanes count for one key
+        const int share = total <= 32 ? 8 : total <= 64 ? 4 : total <= 128 ? 2 : 1;
+        for (int i = tid / share; i < total; i += kRowThreads / share) {
             const uint64_t mine = sel.found[i];
             int place = 0;
-            for (int j = 0; j < total; ++j) {
+#pragma unroll 4
+            for (int j = tid % share; j < total; j += share) {
                 const uint64_t other = sel.found[j];
                 place += other > mine || (other == mine && j < i);
             }
+            for (int off = 1; off < share; off <<= 1) place += __shfl_xor(place, off);
             if (place < want) sel.kept[place] = mine;      // the barrier above: kept has been copied
         }
     } else {
@@ -246,7 +251,7 @@ __device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long 
     const float log_s = logf(sum.s);
     // log p of a logit
     auto model_logp = [&](float v) { return none ? -INFINITY : (v - sum.m) / in.temperature - log_s; };
-    float entropy = none ? 0.f : log_s - kLn2 * (sum.u / sum.s);
+    const float entropy = none ? 0.f : log_s - kLn2 * (sum.u / sum.s);
     const int target = out.targets && tid == 0 ? out.targets[row] : -1;
     const bool wanted = target >= 0 && target < in.vocab;
     if (tid == 0) write_norms(out.norms, row, sum.m, log_s, none);
@@ -380,45 +385,65 @@ __device__ inline void finish_distill(const RowsIn& in, const DistillOut& out, l
 // 16-byte chunks that a thread holds at once
 constexpr int kRowChunks = 4;
 
+// Whole chunks c0, c0 + kRowThreads, ... of a row for a thread's place; from `end` on the last one again.  No branch, so that the
+// loads of the next tile stay in flight while this one is added up.
 template <class T>
 __device__ inline void load_tile(const RowChunks<T>& row, int c0, int end, Chunk<T> (&k)[kRowChunks]) {
-    const int tid = threadIdx.x;
-    if (c0 + kRowChunks * kRowThreads <= end && row.whole(c0) && row.whole(c0 + kRowChunks * kRowThreads - 1)) {
 #pragma unroll
-        for (int i = 0; i < kRowChunks; ++i) k[i].bits = row.base[c0 + i * kRowThreads + tid];
-        return;
-    }
+    for (int i = 0; i < kRowChunks; ++i) k[i].bits = row.base[min(c0 + i * kRowThreads + (int)threadIdx.x, end - 1)];
+}
+
+template <class T>
+__device__ inline void clear(Chunk<T>& k) {
+    float none[Chunk<T>::VEC];
 #pragma unroll
-    for (int i = 0; i < kRowChunks; ++i) {
-        const int c = c0 + i * kRowThreads + tid;
-        if (c < end) k[i] = row.load(c);
-        else {
-            float none[Chunk<T>::VEC];
+    for (int j = 0; j < Chunk<T>::VEC; ++j) none[j] = -INFINITY;
+    k.narrow(none);
+}
+
+// -inf in the place of what load_tile read again
+template <class T>
+__device__ inline void cut_tile(int c0, int end, Chunk<T> (&k)[kRowChunks]) {
+    if (c0 + kRowChunks * kRowThreads <= end) return;
 #pragma unroll
-            for (int j = 0; j < Chunk<T>::VEC; ++j) none[j] = -INFINITY;
-            k[i].narrow(none);
-        }
+    for (int i = 0; i < kRowChunks; ++i)
+        if (c0 + i * kRowThreads + (int)threadIdx.x >= end) clear(k[i]);
+}
+
+// The row's values before its first whole chunk (`front`) and behind its last one (`back`), a chunk in each of the first two
+// threads; -inf elsewhere.  Returns the chunk that it is, for its tokens.
+template <class T>
+__device__ inline int load_edges(const RowChunks<T>& row, bool front, bool back, Chunk<T> (&k)[1]) {
+    clear(k[0]);
+    const int c = threadIdx.x == 0 ? 0 : row.end_whole();
+    if ((threadIdx.x == 0 && front) || (threadIdx.x == 1 && back)) k[0] = row.load(c);
+    return c;
+}
+
+template <class T, int N>
+__device__ inline void largest_of_chunks(const Chunk<T> (&k)[N], float (&most)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float x[Chunk<T>::VEC];
+        k[i].widen(x);
+        most[i] = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < Chunk<T>::VEC; j += 2) most[i] = max3(most[i], x[j], x[j + 1]);
     }
 }
 
 // Adds the chunks to the sums about the thread's own maximum; leaves the maximum of every chunk.
-template <class T, bool ENTROPY>
-__device__ inline void add_tile(Chunk<T> (&k)[kRowChunks], float scale, RowSum& sum, float (&most)[kRowChunks]) {
+template <class T, bool ENTROPY, int N>
+__device__ inline void add_tile(Chunk<T> (&k)[N], float scale, RowSum& sum, float (&most)[N]) {
     constexpr int VEC = Chunk<T>::VEC;
+    largest_of_chunks(k, most);
     float top = sum.m;
 #pragma unroll
-    for (int i = 0; i < kRowChunks; ++i) {
-        float x[VEC];
-        k[i].widen(x);
-        most[i] = x[0];
-#pragma unroll
-        for (int j = 1; j < VEC; ++j) most[i] = fmaxf(most[i], x[j]);
-        top = fmaxf(top, most[i]);
-    }
+    for (int i = 0; i < N; ++i) top = fmaxf(top, most[i]);
     if (top > sum.m) sum.raise(top, scale);
     const float ref = sum.m == -INFINITY ? 0.f : sum.m;     // nothing but -inf so far: t = -inf, not a NaN
 #pragma unroll
-    for (int i = 0; i < kRowChunks; ++i) {
+    for (int i = 0; i < N; ++i) {
         float x[VEC];
         k[i].forget_widened();
         k[i].widen(x);
@@ -431,23 +456,23 @@ __device__ inline void add_tile(Chunk<T> (&k)[kRowChunks], float scale, RowSum& 
     }
 }
 
-template <class T>
-__device__ inline uint64_t best_of_tile(const Chunk<T> (&k)[kRowChunks], const float (&most)[kRowChunks], int first_token) {
+// The largest key of a thread's chunks, 0 if they hold nothing above -inf.
+template <class T, int N>
+__device__ inline uint64_t best_of_tile(Chunk<T> (&k)[N], const float (&most)[N], int first) {
     constexpr int VEC = Chunk<T>::VEC;
-    Chunk<T> best = k[0];
     float top = most[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) top = fmaxf(top, most[i]);
     int at = 0;
 #pragma unroll
-    for (int i = 1; i < kRowChunks; ++i)
-        if (most[i] > top) { best = k[i]; top = most[i]; at = i; }
-    if (!(top > -INFINITY)) return 0;
-    float x[VEC];
-    best.widen(x);
-    int j0 = 0;
+    for (int i = N - 1; i >= 0; --i) {
+        float x[VEC];
+        k[i].forget_widened();
+        k[i].widen(x);
 #pragma unroll
-    for (int j = VEC - 1; j >= 0; --j)
-        if (x[j] == top) j0 = j;
-    return token_key(top, (uint32_t)(first_token + at * kRowThreads * VEC + j0));
+        for (int j = VEC - 1; j >= 0; --j) at = x[j] == top ? i * kRowThreads * VEC + j : at;
+    }
+    return top > -INFINITY ? token_key(top, (uint32_t)(first + at)) : 0;
 }
 
 enum class RowMode { kScore, kScoreTop, kDistill };
@@ -484,20 +509,84 @@ __device__ inline void finish_row(const RowsIn& in, const Out& out, long long ro
     else finish_distill<T>(in, out, row, sum, lds.rows.scratch);
 }
 
-// One workgroup: the chunks [split * chunks, ...) of a row.
+// The keys of a tile that are at least b, b = 0 for all but -inf
+template <class T, int N, class Push>
+__device__ inline void scan_tile(Chunk<T> (&k)[N], const float (&most)[N], int first, uint64_t b, Push&& push) {
+    constexpr int VEC = Chunk<T>::VEC;
+    const float least = b ? key_value(b) : -INFINITY;
+    asm volatile("" : "+v"(first));                        // tokens are formed where they are needed, not kept in registers
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (!(most[i] >= least)) continue;
+        float x[VEC];
+        k[i].forget_widened();
+        k[i].widen(x);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+            if (x[j] >= least && x[j] > -INFINITY) {
+                const uint64_t key = token_key(x[j], (uint32_t)(first + i * kRowThreads * VEC + j));
+                if (key >= b) push(key);
+            }
+    }
+}
+
+// The best keys of chunks [begin, end), whole or not, for rows where too many keys passed the bounds of the one pass: a chunk a
+// thread at a time, each time bounded by the best of these while too few keys are kept.
+template <class T>
+__device__ inline int select_step_by_step(const RowChunks<T>& row, int begin, int end, int want, Selection& sel) {
+    uint64_t bound = 0;
+    int n_kept = 0;
+    for (int c0 = begin; c0 < end; c0 += kRowThreads) {
+        const int c = c0 + (int)threadIdx.x, first = c * Chunk<T>::VEC - row.lead;
+        Chunk<T> k[1];
+        float most[1];
+        if (c < end) k[0] = row.load(c);
+        else clear(k[0]);
+        largest_of_chunks(k, most);
+        if (n_kept < want) bound = bound_of_best(sel, best_of_tile(k, most, first), want);
+        n_kept = take_candidates(sel, bound, n_kept, want, [&](uint64_t b, auto push) { scan_tile(k, most, first, b, push); });
+    }
+    return n_kept;
+}
+
+// One workgroup: the whole chunks [split * chunks, ...) of a row; the row's first workgroup takes what lies before them too, and
+// its last one what lies behind.
+//
+// Alternatives: the first tile's keys above a bound from its lanes' best are merged at once, and what passes the want-th of
+// those is collected from the next tiles without a barrier, merged after 4, 16, ... tiles (a bound from N tiles lets about as
+// many of the next N pass as are wanted).
 template <class T, RowMode MODE, class Out>
-__global__ __launch_bounds__(kRowThreads, 4) void row_statistics_kernel(RowsIn in, RowSplit split, Out out) {
+__global__ __launch_bounds__(kRowThreads, 5) void row_statistics_kernel(RowsIn in, RowSplit split, Out out) {
     constexpr int VEC = Chunk<T>::VEC;
     constexpr bool TOP = MODE == RowMode::kScoreTop, ENTROPY = MODE != RowMode::kDistill;
     __shared__ RowLds<MODE> lds;
     const long long r = blockIdx.x / (unsigned)split.splits;
     const int part = blockIdx.x % (unsigned)split.splits;
     const RowChunks<T> row(in.data, r, in.stride, in.vocab);
-    const int begin = part * split.chunks;
-    const int end = min(begin + split.chunks, row.count());
+    const int begin = row.first_whole() + part * split.chunks;
+    const int end = min(begin + split.chunks, row.end_whole());
+    const bool last = part + 1 == split.splits;
+    const bool front = part == 0 && !row.whole(0), back = last && row.end_whole() > 0 && row.end % VEC;
     RowSum sum;
     uint64_t bound = 0;
-    int n_kept = 0, want = 0;
+    int n_kept = 0, want = 0, tiles = 0, merge_at = 1;
+    bool many = false;                                     // more candidates than there is room for
+    auto collect = [&](uint64_t key) {
+        if constexpr (TOP) {
+            const int at = atomicAdd(&lds.sel.n_found, 1);         // the order of arrival does not matter: keys are sorted
+            if (at < kCandidates) lds.sel.found[at] = key;
+        }
+    };
+    auto merge = [&] {
+        if constexpr (TOP) {
+            __syncthreads();
+            const int n = lds.sel.n_found;
+            __syncthreads();
+            many = n > kCandidates;
+            if (n > 0 && !many) n_kept = keep_best(lds.sel, n, n_kept, want);
+            if (n_kept == want) bound = lds.sel.kept[want - 1];
+        }
+    };
     if constexpr (TOP) {
         want = out.want;
         if (threadIdx.x == 0) lds.sel.n_found = 0;
@@ -507,33 +596,39 @@ __global__ __launch_bounds__(kRowThreads, 4) void row_statistics_kernel(RowsIn i
     if (begin < end) load_tile(row, begin, end, now);
     for (int c0 = begin; c0 < end; c0 += kRowChunks * kRowThreads) {
         const int c1 = c0 + kRowChunks * kRowThreads;
-        if (c1 < end) load_tile(row, c1, end, next);
+        load_tile(row, c1, end, next);
+        cut_tile(c0, end, now);
         float most[kRowChunks];
         add_tile<T, ENTROPY>(now, in.scale, sum, most);
         if constexpr (TOP) {
             const int first = (c0 + (int)threadIdx.x) * VEC - row.lead;
-            if (n_kept < want) bound = bound_of_best(lds.sel, best_of_tile(now, most, first), want);
-            n_kept = take_candidates(lds.sel, bound, n_kept, want, [&](uint64_t b, auto push) {
-                const float least = b ? key_value(b) : -INFINITY;
-                int token0 = first;
-                asm volatile("" : "+v"(token0));           // tokens are formed where they are needed, not kept in registers
-#pragma unroll
-                for (int i = 0; i < kRowChunks; ++i) {
-                    if (!(most[i] >= least)) continue;
-                    float x[VEC];
-                    now[i].forget_widened();
-                    now[i].widen(x);
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j)
-                        if (x[j] >= least && x[j] > -INFINITY) {
-                            const uint64_t key = token_key(x[j], (uint32_t)(token0 + i * kRowThreads * VEC + j));
-                            if (key >= b) push(key);
-                        }
+            if (c0 == begin) bound = bound_of_best(lds.sel, best_of_tile(now, most, first), want);
+            if (!many) {
+                scan_tile(now, most, first, bound, collect);
+                if (++tiles == merge_at) {
+                    merge_at *= 4;
+                    merge();
                 }
-            });
+            }
         }
 #pragma unroll
         for (int i = 0; i < kRowChunks; ++i) now[i] = next[i];
+    }
+    if (front || back) {
+        Chunk<T> k[1];
+        float most[1];
+        const int first = load_edges(row, front, back, k) * VEC - row.lead;
+        add_tile<T, ENTROPY>(k, in.scale, sum, most);
+        if (TOP && !many) scan_tile(k, most, first, bound, collect);
+    }
+    if constexpr (TOP) {
+        if (!many) merge();
+        if (many) {
+            __syncthreads();
+            if (threadIdx.x == 0) lds.sel.n_found = 0;
+            __syncthreads();
+            n_kept = select_step_by_step(row, part == 0 ? 0 : min(begin, end), last ? row.count() : end, want, lds.sel);
+        }
     }
     sum = block_join(sum, in.scale, lds.rows);
     if (split.splits == 1) {
@@ -561,9 +656,15 @@ __global__ __launch_bounds__(kRowThreads) void row_join_kernel(RowsIn in, RowSpl
         const uint64_t* keys = split.keys + r * split.splits * (long long)want;
         // every workgroup's q-th largest key bounds q keys from below; together splits * q >= want
         const int q = (want + split.splits - 1) / split.splits;
+        static_assert(kMostSplits <= 64, "one wave reads them all");
         uint64_t low = ~(uint64_t)0, high = 0;
-        for (int p = 0; p < split.splits; ++p) {
-            const uint64_t a = keys[(long long)p * want + q - 1], b = keys[(long long)p * want + want - 1];
+        const int p = threadIdx.x & 63;
+        if (p < split.splits) {
+            low = keys[(long long)p * want + q - 1];
+            high = keys[(long long)p * want + want - 1];
+        }
+        for (int off = 32; off; off >>= 1) {
+            const uint64_t a = __shfl_xor((unsigned long long)low, off), b = __shfl_xor((unsigned long long)high, off);
             low = a < low ? a : low;
             high = b > high ? b : high;
         }

@@ -74,12 +74,14 @@ struct RowChunks {
     int lead, end;                   // elements [lead, end) are the row's
     __device__ RowChunks(const void* data, long long r, long long stride, int count) {
         row = reinterpret_cast<const T*>(data) + r * stride;
-        const uintptr_t at = reinterpret_cast<uintptr_t>(row);
-        base = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
-        lead = (int)((at & 15) / sizeof(T));
+        lead = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+        base = reinterpret_cast<const uint4*>(row - lead);       // by pointer arithmetic, so that its loads are known to be of global memory
         end = lead + count;
     }
     __device__ inline int count() const { return (end + VEC - 1) / VEC; }
+    // chunks [first_whole, end_whole) lie inside of the row; the one before and the one behind hold the rest of it
+    __device__ inline int first_whole() const { return lead ? 1 : 0; }
+    __device__ inline int end_whole() const { return end / VEC; }
     __device__ inline bool whole(int c) const { return c * VEC >= lead && (c + 1) * VEC <= end; }
     __device__ inline float value(int v) const { return (float)row[v]; }
     // `fill` stands for values outside of the row
@@ -101,6 +103,14 @@ struct RowChunks {
 };
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }       // results under 2^-126 are 0
+
+// The largest of three; NaNs are passed over.  (fmaxf of values that come from integer operations costs a second instruction each, which
+// makes quiet a signalling NaN.)
+__device__ inline float max3(float a, float b, float c) {
+    float d;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    return d;
+}
 
 // The sum over a workgroup of THREADS, in every thread; the order of additions is fixed.  `scratch`: THREADS / 64 words that no
 // wave still reads; they are free again after the next barrier.
