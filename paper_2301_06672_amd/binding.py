@@ -142,7 +142,8 @@ def _dp(t: Optional[torch.Tensor]):
 
 
 def _stream():
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # the current stream's handle; torch.cuda.current_stream() makes an object for it first, which takes longer than a launch
+    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
 
 
 def _dev_f32(x) -> torch.Tensor:

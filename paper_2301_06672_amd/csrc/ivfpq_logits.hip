@@ -22,6 +22,7 @@ namespace {
 
 constexpr int kRowThreads = 256, kRowWaves = kRowThreads / 64;
 constexpr int kMostSplits = 64;                            // workgroups that share a row
+constexpr int kMostSplitsTop = 16;                         // ... and where each leaves a list of its best keys: fewer lists are joined faster
 constexpr int kMostTop = IVFPQ_MAX_MIXED;                  // keys a selection keeps
 constexpr int kCandidates = 2048 - kMostTop;               // ... and takes in before it sorts
 constexpr float kLeastPower = -150.f;                      // 2^t is 0 in fp32 below this: t is cut there before t 2^t
@@ -80,7 +81,7 @@ __device__ inline float key_value(uint64_t key) { return ordered_key_value((uint
 __device__ inline int key_token(uint64_t key) { return (int)~(uint32_t)key; }
 
 struct Selection {
-    uint64_t found[kCandidates + kMostTop];    // candidates, then room for the kept ones
+    alignas(16) uint64_t found[kCandidates + kMostTop];    // candidates, then room for the kept ones
     uint64_t kept[kMostTop];                   // the largest so far, descending
     uint64_t wave_bound[2][kRowWaves];
     int n_found;
@@ -109,16 +110,24 @@ __device__ inline int keep_best(Selection& sel, int n, int n_kept, int want) {
     const int total = n + n_kept;
     const int keep = total < want ? total : want;
     if (total <= 2 * kRowThreads) {
-        __syncthreads();
-        // `share` neighbouring lanes count for one key
+        // `share` neighbouring lanes count for one key; eight keys a lane are read at once, none (0) behind the last
         const int share = total <= 32 ? 8 : total <= 64 ? 4 : total <= 128 ? 2 : 1;
+        const int padded = (total + 8 * share - 1) / (8 * share) * (8 * share);
+        for (int i = total + tid; i < padded; i += kRowThreads) sel.found[i] = 0;
+        __syncthreads();
         for (int i = tid / share; i < total; i += kRowThreads / share) {
             const uint64_t mine = sel.found[i];
             int place = 0;
-#pragma unroll 4
-            for (int j = tid % share; j < total; j += share) {
-                const uint64_t other = sel.found[j];
-                place += other > mine || (other == mine && j < i);
+            for (int j0 = tid % share * 2; j0 < padded; j0 += 8 * share) {
+                uint64_t other[8];
+#pragma unroll
+                for (int o = 0; o < 8; o += 2) {
+                    const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(&sel.found[j0 + o * share]);
+                    other[o] = two.x;
+                    other[o + 1] = two.y;
+                }
+#pragma unroll
+                for (int o = 0; o < 8; ++o) place += other[o] > mine;
             }
             for (int off = 1; off < share; off <<= 1) place += __shfl_xor(place, off);
             if (place < want) sel.kept[place] = mine;      // the barrier above: kept has been copied
@@ -222,7 +231,7 @@ struct DistillOut {
 };
 
 struct MixShared {
-    int token[IVFPQ_MAX_LISTED];
+    alignas(16) int token[IVFPQ_MAX_LISTED];
     float logp[IVFPQ_MAX_LISTED];     // of the mixture
     double sums[kRowWaves];
     float hit, model, near;           // the target's log-probability if it is listed; log weights in this row
@@ -280,6 +289,7 @@ __device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long 
         mix.token[j] = used ? token : -1;
         any |= used;
     }
+    for (int j = k + tid; j < (k + 15) / 16 * 16; j += kRowThreads) mix.token[j] = -1;
     any = __syncthreads_or(any);
     const float log_model = none ? -INFINITY : any ? out.log_model : 0.f;
     const float log_near = !any ? -INFINITY : none ? 0.f : out.log_near;
@@ -318,7 +328,13 @@ __device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long 
         for (int i = tid; i < n_kept; i += kRowThreads) {
             const int token = key_token(sel->kept[i]);
             bool listed = false;
-            for (int j = 0; j < k; ++j) listed |= mix.token[j] == token;
+            for (int j = 0; j < k; j += 16) {              // -1 behind the last
+                int4 some[4];
+#pragma unroll
+                for (int o = 0; o < 4; ++o) some[o] = *reinterpret_cast<const int4*>(&mix.token[j + 4 * o]);
+#pragma unroll
+                for (int o = 0; o < 4; ++o) listed |= some[o].x == token || some[o].y == token || some[o].z == token || some[o].w == token;
+            }
             const float logp = log_model + model_logp(key_value(sel->kept[i]));
             if (!listed && logp > -INFINITY) sel->found[atomicAdd(&sel->n_found, 1)] = token_key(logp, (uint32_t)token);
         }
@@ -327,10 +343,11 @@ __device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long 
                 sel->found[atomicAdd(&sel->n_found, 1)] = token_key(mix.logp[j], (uint32_t)mix.token[j]);
         __syncthreads();
         const int n = sel->n_found;
+        if (tid < out.top) sel->kept[tid] = 0;             // a token listed twice, which a caller should not, leaves a place unused
         __syncthreads();
         const int best = keep_best(*sel, n, 0, out.top);
         for (int i = tid; i < out.top; i += kRowThreads) {
-            const bool used = i < best;
+            const bool used = i < best && sel->kept[i];
             out.top_tokens[row * out.top + i] = used ? key_token(sel->kept[i]) : -1;
             out.top_logprobs[row * out.top + i] = used ? key_value(sel->kept[i]) : -INFINITY;
         }
@@ -672,9 +689,15 @@ __global__ __launch_bounds__(kRowThreads) void row_join_kernel(RowsIn in, RowSpl
         if (threadIdx.x == 0) lds.sel.n_found = 0;
         __syncthreads();
         n_kept = take_candidates(lds.sel, bound, 0, want, [&](uint64_t b, auto push) {
-            for (int i = threadIdx.x; i < split.splits * want; i += kRowThreads) {
-                const uint64_t key = keys[i];
-                if (key >= b && key) push(key);
+            constexpr int kAhead = 8;                      // loads in flight: this kernel is little more than their latency
+            const int n = split.splits * want;
+            for (int i = threadIdx.x; i < n; i += kAhead * kRowThreads) {
+                uint64_t some[kAhead];
+#pragma unroll
+                for (int o = 0; o < kAhead; ++o) some[o] = i + o * kRowThreads < n ? keys[i + o * kRowThreads] : 0;
+#pragma unroll
+                for (int o = 0; o < kAhead; ++o)
+                    if (some[o] >= b && some[o]) push(some[o]);
             }
         });
     }
@@ -873,18 +896,18 @@ size_t split_bytes(int64_t n, const RowSplit& s, int want) {
 
 // the largest over the value types
 size_t row_workspace(int64_t n, int32_t vocab, int want) {
+    const int most = want ? kMostSplitsTop : kMostSplits;
     if (n < 1 || vocab < 1 || vocab > (1 << 30) || n > kMostRows) return 0;
-    return std::max(split_bytes(n, split_rows(n, vocab, 4, kMostSplits), want), split_bytes(n, split_rows(n, vocab, 8, kMostSplits), want));
+    return std::max(split_bytes(n, split_rows(n, vocab, 4, most), want), split_bytes(n, split_rows(n, vocab, 8, most), want));
 }
 
 template <class T, RowMode MODE, class Out>
-int launch_rows(int64_t n, const RowsIn& in, const Out& out, int want, void* ws, hipStream_t stream) {
-    RowSplit s = split_rows(n, in.vocab, Chunk<T>::VEC, kMostSplits);
+int launch_rows(int64_t n, const RowsIn& in, const Out& out, void* ws, hipStream_t stream) {
+    RowSplit s = split_rows(n, in.vocab, Chunk<T>::VEC, MODE == RowMode::kScoreTop ? kMostSplitsTop : kMostSplits);
     if (s.splits > 1) {
         s.partials = (Partial*)ws;
         s.keys = (uint64_t*)((char*)ws + align_up((size_t)n * s.splits * sizeof(Partial)));
     }
-    (void)want;
     hipLaunchKernelGGL((row_statistics_kernel<T, MODE, Out>), dim3((unsigned)(n * s.splits)), dim3(kRowThreads), 0, stream, in, s, out);
     HIP_TRY(hipGetLastError());
     if (s.splits > 1) {
@@ -928,8 +951,8 @@ int token_logprobs(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab
                        d_logprobs, d_entropy, d_norms, d_top_tokens, d_top_logprobs};
     return with_value_type(dtype, [&](auto v) {
         using T = decltype(v);
-        if (top) return launch_rows<T, RowMode::kScoreTop>(n, in, out, want, d_workspace, (hipStream_t)hip_stream);
-        return launch_rows<T, RowMode::kScore>(n, in, out, want, d_workspace, (hipStream_t)hip_stream);
+        if (top) return launch_rows<T, RowMode::kScoreTop>(n, in, out, d_workspace, (hipStream_t)hip_stream);
+        return launch_rows<T, RowMode::kScore>(n, in, out, d_workspace, (hipStream_t)hip_stream);
     });
 }
 
@@ -937,7 +960,7 @@ int distill_forward(const char* what, const RowsIn& in, int32_t dtype, int64_t n
                     void* d_workspace, hipStream_t stream) {
     const DistillOut out{teacher, d_loss, d_norms};
     return with_value_type(dtype, [&](auto v) {
-        return launch_rows<decltype(v), RowMode::kDistill>(n, in, out, 0, d_workspace, stream);
+        return launch_rows<decltype(v), RowMode::kDistill>(n, in, out, d_workspace, stream);
     });
 }
 
