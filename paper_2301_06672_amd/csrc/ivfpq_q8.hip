@@ -96,7 +96,7 @@ struct Product {
     int m, n, k;
 };
 
-__device__ inline float scaled(const Product& p, int acc, float sa, float sb, float bias) { return (sa * sb) * (float)acc + bias; }
+__device__ inline float scaled(int acc, float sa, float sb, float bias) { return (sa * sb) * (float)acc + bias; }
 
 // Bytes [at, at + 16) of a row, 0 from k on: a sum takes nothing of what lies there.
 __device__ inline intx4 masked16(const int8_t* row, int at, int k) {
@@ -186,7 +186,7 @@ __global__ __launch_bounds__(256) void skinny_kernel(Product p) {
                 const int i = i0 + 16 * s + 4 * (lane >> 4) + v;
                 const int at = (s * NT + t) * 4 + v;
                 const int sum = acc[s][t][v] + sums[0][at][lane] + sums[1][at][lane] + sums[2][at][lane];
-                if (i < p.m) reinterpret_cast<T*>(p.out)[i * p.out_stride + j] = (T)scaled(p, sum, p.a_scales[i], sb, bias);
+                if (i < p.m) reinterpret_cast<T*>(p.out)[i * p.out_stride + j] = (T)scaled(sum, p.a_scales[i], sb, bias);
             }
     }
 }
@@ -194,8 +194,20 @@ __global__ __launch_bounds__(256) void skinny_kernel(Product p) {
 // Many rows of a: a tile of BM x BN outputs a workgroup of WM x WN waves, operands through the LDS in slices of 128 bytes of
 // the rows, two slices in turn: one is loaded straight into the LDS while the other is multiplied, one barrier a slice.
 // v_mfma_i32_32x32x32_i8: lane L brings row / column L % 32 and bytes [16 (L / 32), ...) of each 32; register v of lane L
-// holds row 8 (v / 4) + 4 (L / 32) + v % 4, column L % 32.  In the LDS the 16-byte pieces of row r stand in the order
-// piece ^ (r % 8), so that eight lanes that read the same piece of consecutive rows use all banks.
+// holds row 8 (v / 4) + 4 (L / 32) + v % 4, column L % 32.  Two rows of 128 bytes cover the 64 banks of the LDS, so the 16-byte
+// pieces of row r stand in the order piece ^ (r / 2 % 8): sixteen lanes that read one piece of sixteen rows use every bank
+// once.
+__device__ inline int piece_at(int row, int piece) { return piece ^ ((row >> 1) & 7); }
+
+// Sums on their way out: rows of BN words and 8 more, which puts rows four apart into opposite halves of the banks
+template <int BN> constexpr int kStagePitch = BN + 8;
+template <int BN, int WM> constexpr size_t kStageBytes = (size_t)WM * 32 * kStagePitch<BN> * sizeof(int);
+
+// 16 bytes a lane straight into the LDS, 1024 from `to` on in the order of the lanes
+__device__ inline void load_piece(const int8_t* base, uint32_t offset, int8_t* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(base + offset), (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
 template <class T, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     constexpr int WAVES = WM * WN, SM = BM / (32 * WM), SN = BN / (32 * WN);
@@ -203,32 +215,46 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int tiles_n = (p.n + BN - 1) / BN;
-    const int i0 = (blockIdx.x / tiles_n) * BM, j0 = (blockIdx.x % tiles_n) * BN;
+    const int i0 = (int)(blockIdx.x / (unsigned)tiles_n) * BM, j0 = (int)(blockIdx.x % (unsigned)tiles_n) * BN;
     constexpr int SLICE = (BM + BN) * 128;
-    // a wave loads eight rows of a slice at a time: lane L the piece that stands at L % 8 in row L / 8
-    const int sub = lane >> 3, piece = (lane & 7) ^ sub;
+    // a wave loads eight rows of a slice at a time: lane L the piece that stands at L % 8 in row L / 8 of them
+    const int sub = lane >> 3;
     const int slices = (p.k + 127) / 128;
-    auto load_rows = [&](const int8_t* rows, long long stride, int first, int count, int n_rows, int k0, int8_t* to) {
-        for (int g = wave; g < n_rows / 8; g += WAVES) {
-            const int r = min(first + g * 8 + sub, count - 1);
-            int at = k0 + piece * 16;
-            at = at < p.k ? at : k0;                       // beyond the row: any of its bytes, the other operand has zeros there
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(rows + r * stride + at),
-                                             (__attribute__((address_space(3))) void*)(to + g * 1024), 16, 0, 0);
-        }
-    };
-    auto load_rows_cut = [&](const int8_t* rows, long long stride, int first, int count, int n_rows, int k0, int8_t* to) {
-        for (int g = wave; g < n_rows / 8; g += WAVES) {
-            const int r = min(first + g * 8 + sub, count - 1);
-            *reinterpret_cast<intx4*>(to + g * 1024 + lane * 16) = masked16(rows + r * stride, k0 + piece * 16, p.k);
-        }
-    };
+    // where a lane's pieces begin, from the tile's first row (rows beyond the last one: the last one again)
+    constexpr int LA = BM / 8 / WAVES, LB = BN / 8 / WAVES;
+    const int8_t* from_a = p.a + i0 * p.a_stride;
+    const int8_t* from_b = p.b + j0 * p.b_stride;
+    uint32_t off_a[LA], off_b[LB];
+#pragma unroll
+    for (int t = 0; t < LA; ++t) {
+        const int r = (t * WAVES + wave) * 8 + sub;
+        off_a[t] = (uint32_t)min(r, p.m - 1 - i0) * (uint32_t)p.a_stride + piece_at(r, lane & 7) * 16;
+    }
+#pragma unroll
+    for (int t = 0; t < LB; ++t) {
+        const int r = (t * WAVES + wave) * 8 + sub;
+        off_b[t] = (uint32_t)min(r, p.n - 1 - j0) * (uint32_t)p.b_stride + piece_at(r, lane & 7) * 16;
+    }
     auto load_slice = [&](int s) {
-        int8_t* to = lds + (s & 1) * SLICE;
+        int8_t* to = lds + (s & 1) * SLICE + wave * 1024;
         const int k0 = s * 128;
-        if (k0 + 128 <= p.k) load_rows(p.a, p.a_stride, i0, p.m, BM, k0, to);
-        else load_rows_cut(p.a, p.a_stride, i0, p.m, BM, k0, to);
-        load_rows(p.b, p.b_stride, j0, p.n, BN, k0, to + BM * 128);
+        if (k0 + 128 <= p.k) {
+#pragma unroll
+            for (int t = 0; t < LA; ++t) load_piece(from_a + k0, off_a[t], to + t * WAVES * 1024);
+#pragma unroll
+            for (int t = 0; t < LB; ++t) load_piece(from_b + k0, off_b[t], to + BM * 128 + t * WAVES * 1024);
+        } else {                                           // the last slice, cut at k
+#pragma unroll
+            for (int t = 0; t < LA; ++t) {
+                const int at = piece_at((t * WAVES + wave) * 8 + sub, lane & 7) * 16;
+                *reinterpret_cast<intx4*>(to + t * WAVES * 1024 + lane * 16) = masked16(from_a + off_a[t] - at, k0 + at, p.k);
+            }
+#pragma unroll
+            for (int t = 0; t < LB; ++t) {
+                const int at = piece_at((t * WAVES + wave) * 8 + sub, lane & 7) * 16;
+                *reinterpret_cast<intx4*>(to + BM * 128 + t * WAVES * 1024 + lane * 16) = masked16(from_b + off_b[t] - at, k0 + at, p.k);
+            }
+        }
     };
     intx16 acc[SM][SN] = {};
     const int l32 = lane & 31, half = lane >> 5;
@@ -237,33 +263,72 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
         __syncthreads();
         if (s + 1 < slices) load_slice(s + 1);
         const int8_t* at = lds + (s & 1) * SLICE;
+        const int8_t* at_a = at + (wm * SM * 32 + l32) * 128;
+        const int8_t* at_b = at + (BM + wn * SN * 32 + l32) * 128;
+        // the operands of a step are read while the step before it is multiplied
+        intx4 va[2][SM], vb[2][SN];
+        auto read = [&](int step) {
+            const int stands = piece_at(l32, 2 * step + half) * 16;
+#pragma unroll
+            for (int t = 0; t < SM; ++t) va[step & 1][t] = *reinterpret_cast<const intx4*>(at_a + t * 32 * 128 + stands);
+#pragma unroll
+            for (int t = 0; t < SN; ++t) vb[step & 1][t] = *reinterpret_cast<const intx4*>(at_b + t * 32 * 128 + stands);
+        };
+        read(0);
 #pragma unroll
         for (int step = 0; step < 4; ++step) {
-            intx4 va[SM], vb[SN];
-            const int stands = ((2 * step + half) ^ (l32 & 7)) * 16;
-#pragma unroll
-            for (int t = 0; t < SM; ++t) va[t] = *reinterpret_cast<const intx4*>(at + (wm * SM * 32 + t * 32 + l32) * 128 + stands);
-#pragma unroll
-            for (int t = 0; t < SN; ++t) vb[t] = *reinterpret_cast<const intx4*>(at + (BM + wn * SN * 32 + t * 32 + l32) * 128 + stands);
+            if (step < 3) read(step + 1);
 #pragma unroll
             for (int x = 0; x < SM; ++x)
 #pragma unroll
-                for (int y = 0; y < SN; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_32x32x32_i8(va[x], vb[y], acc[x][y], 0, 0, 0);
+                for (int y = 0; y < SN; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_32x32x32_i8(va[step & 1][x], vb[step & 1][y], acc[x][y], 0, 0, 0);
         }
-    }
-    T* out = reinterpret_cast<T*>(p.out);
+        __builtin_amdgcn_sched_group_barrier(0x100, SM + SN, 0);           // the first step's reads, then a read behind every product
 #pragma unroll
-    for (int y = 0; y < SN; ++y) {
-        const int j = j0 + (wn * SN + y) * 32 + l32;
-        if (j >= p.n) continue;
-        const float sb = p.b_scales[j], bias = p.bias ? p.bias[j] : 0.f;
+        for (int step = 0; step < 3; ++step) {
 #pragma unroll
-        for (int x = 0; x < SM; ++x)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int i = i0 + (wm * SM + x) * 32 + 8 * (v / 4) + 4 * half + v % 4;
-                if (i < p.m) out[i * p.out_stride + j] = (T)scaled(p, acc[x][y][v], p.a_scales[i], sb, bias);
+            for (int o = 0; o < SM + SN; ++o) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
+            if (SM * SN > SM + SN) __builtin_amdgcn_sched_group_barrier(0x008, SM * SN - SM - SN, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, SM * SN, 0);
+    }
+    // The sums pass through the LDS, 32 rows of every wave at a time, so that a thread scales and stores 16 bytes of a row and a
+    // row of the tile is written in one piece.
+    constexpr int VEC = 16 / sizeof(T), PER_ROW = BN / VEC, AT_ONCE = 64 * WAVES / PER_ROW;
+    typedef T piece_t __attribute__((ext_vector_type(VEC), aligned(sizeof(T))));
+    int* stage = reinterpret_cast<int*>(lds);
+    const int col = (int)threadIdx.x % PER_ROW * VEC, j = j0 + col;
+    float sb[VEC], bias[VEC];
+#pragma unroll
+    for (int o = 0; o < VEC; ++o) {
+        sb[o] = j + o < p.n ? p.b_scales[j + o] : 0.f;
+        bias[o] = p.bias && j + o < p.n ? p.bias[j + o] : 0.f;
+    }
+#pragma unroll
+    for (int x = 0; x < SM; ++x) {
+        __syncthreads();
+#pragma unroll
+        for (int y = 0; y < SN; ++y)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                stage[(wm * 32 + 8 * (v / 4) + 4 * half + v % 4) * kStagePitch<BN> + (wn * SN + y) * 32 + l32] = acc[x][y][v];
+        __syncthreads();
+#pragma unroll
+        for (int r = (int)threadIdx.x / PER_ROW; r < WM * 32; r += AT_ONCE) {
+            const int i = i0 + (r / 32 * SM + x) * 32 + r % 32;
+            if (i >= p.m || j >= p.n) continue;
+            const float sa = p.a_scales[i];
+            T* out = reinterpret_cast<T*>(p.out) + i * p.out_stride + j;
+            piece_t y;
+#pragma unroll
+            for (int o = 0; o < VEC; ++o) y[o] = (T)scaled(stage[r * kStagePitch<BN> + col + o], sa, sb[o], bias[o]);
+            if (j + VEC <= p.n) *reinterpret_cast<piece_t*>(out) = y;
+            else
+                for (int o = 0; j + o < p.n; ++o) out[o] = y[o];
+        }
     }
 }
 
@@ -277,7 +342,7 @@ int launch_skinny(const Product& p, hipStream_t stream) {
 
 template <class T, int BM, int BN, int WM, int WN>
 int launch_tiles(const Product& p, hipStream_t stream) {
-    constexpr size_t lds = 2 * (BM + BN) * 128;
+    const size_t lds = std::max((size_t)(p.k > 128 ? 2 : 1) * (BM + BN) * 128, kStageBytes<BN, WM>);
     const int64_t tiles = (int64_t)((p.m + BM - 1) / BM) * ((p.n + BN - 1) / BN);
     if (tiles * (64 * WM * WN) > 0xFFFFFFFFll) return fail(IVFPQ_EUNSUPPORTED, "ivfpq_q8_matmul: m=%d n=%d is over 2^32 threads", p.m, p.n);
     if (int s = allow_full_lds(tile_kernel<T, BM, BN, WM, WN>)) return s;
@@ -293,7 +358,7 @@ int launch_product(const Product& p, hipStream_t stream) {
     if (p.m <= 16) return launch_skinny<T, 1, 1>(p, stream);
     if (p.m <= 32) return launch_skinny<T, 2, 1>(p, stream);
     if (p.m <= 64) return launch_skinny<T, 4, 1>(p, stream);
-    if ((int64_t)((p.m + 255) / 256) * ((p.n + 255) / 256) >= 256) return launch_tiles<T, 256, 256, 2, 4>(p, stream);
+    if (p.k > 256 && (int64_t)((p.m + 255) / 256) * ((p.n + 255) / 256) >= 256) return launch_tiles<T, 256, 256, 2, 4>(p, stream);
     return launch_tiles<T, 128, 128, 2, 2>(p, stream);
 }
 
