@@ -270,7 +270,7 @@ int ivfpq_refine(const float* d_data, int64_t n_data, int32_t d, const float* d_
  *  - Matrices have rows of contiguous values, `stride` values (not bytes) from one row to the next; pointers and
  *    strides need the alignment of a value only, unless stated.  `dtype` is an ivfpq_values_dtype_t.  Logits and 16-bit
  *    rows are widened to fp32; sums, maxima and statistics are fp32; a result in 16 bits is rounded once, to nearest.
- *  - A call takes up to 2^23 rows of logits of up to 2^30 tokens.
+ *  - A call takes up to 2^21 rows of logits of up to 2^30 tokens.
  *  - A token is an int32 in [0, vocab); any other value marks an unused place.
  *  - With T = temperature, 1e-6 <= T <= 1e6, a row of logits x has the distribution p_v = exp((x_v - M)/T) / sum_u exp((x_u - M)/T),
  *    M its largest logit.  A logit of -inf has p = 0; a logit of the type's lowest value is a number like any other.  A row

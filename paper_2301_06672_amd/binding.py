@@ -198,44 +198,50 @@ class TokenLogprobs(NamedTuple):
     top_logprobs: Optional[torch.Tensor]   # [n][top]
 
 
-def _need(ok: bool, message: str):
-    if not ok:
-        raise IvfpqError(EINVAL, message)
+def _refuse(message: str):
+    raise IvfpqError(EINVAL, message)
 
 
 def _on_device(what: str, *tensors):
     device = torch.cuda.current_device()
     for t in tensors:
-        _need(t is None or (isinstance(t, torch.Tensor) and t.is_cuda and t.device.index == device),
-              f"{what}: a tensor is not on the current CUDA device")
+        if t is not None and not (isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() == device):
+            _refuse(f"{what}: a tensor is not on the current CUDA device")
 
 
-def _plain(what: str, t: torch.Tensor, dtype, shape):
+def _plain(what: str, t: torch.Tensor, dtype, *shape):
     """A contiguous tensor of this type and shape."""
-    _need(t.dtype == dtype and tuple(t.shape) == tuple(shape), f"{what}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if t.dtype != dtype or t.shape != shape:
+        _refuse(f"{what}: expected {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
     return t.contiguous()
 
 
 def _value_rows(what: str, x: torch.Tensor) -> torch.Tensor:
-    _need(x.dim() == 2 and x.dtype in VALUES_DTYPES, f"{what}: expected a matrix of float32, float16 or bfloat16, got {x.dtype} {tuple(x.shape)}")
+    if x.dim() != 2 or x.dtype not in VALUES_DTYPES:
+        _refuse(f"{what}: expected a matrix of float32, float16 or bfloat16, got {x.dtype} {tuple(x.shape)}")
+    return x if _rows_apart(x) else x.contiguous()
+
+
+def _rows_apart(x: torch.Tensor) -> bool:
+    """Whether a row's values are contiguous and rows do not overlap."""
     n, d = x.shape
-    return x if (d <= 1 or x.stride(1) == 1) and (n <= 1 or x.stride(0) >= d) else x.contiguous()
+    return (d <= 1 or x.stride(1) == 1) and (n <= 1 or x.stride(0) >= d)
 
 
 def _grad_like(what: str, logits: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
     if out is None:
         return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
     _on_device(what, out)
-    n, d = logits.shape
-    _need(out.shape == logits.shape and out.dtype == logits.dtype and (d <= 1 or out.stride(1) == 1) and (n <= 1 or out.stride(0) >= d),
-          f"{what}: out has another shape, type or layout than the logits")
+    if out.shape != logits.shape or out.dtype != logits.dtype or not _rows_apart(out):
+        _refuse(f"{what}: out has another shape, type or layout than the logits")
     return out
 
 
 def _listed(what: str, tokens: torch.Tensor, values: torch.Tensor, n: int):
-    _need(tokens.dim() == 2, f"{what}: listed tokens are a matrix")
-    shape = (n, tokens.shape[1])
-    return _plain(what, tokens, torch.int32, shape), _plain(what, values, torch.float32, shape)
+    if tokens.dim() != 2:
+        _refuse(f"{what}: listed tokens are a matrix")
+    k = tokens.shape[1]
+    return _plain(what, tokens, torch.int32, n, k), _plain(what, values, torch.float32, n, k)
 
 
 def _scratch(nbytes: int) -> Optional[torch.Tensor]:
@@ -259,7 +265,8 @@ def ivfpq_quantize_rows(rows: torch.Tensor):
 
 def _code_rows(what: str, codes: torch.Tensor):
     """-> (codes, row stride): rows of 16-byte pieces that can all be read, as ivfpq_quantize_rows makes them; other layouts are copied."""
-    _need(codes.dim() == 2 and codes.dtype == torch.int8, f"{what}: codes are a matrix of int8, got {codes.dtype} {tuple(codes.shape)}")
+    if codes.dim() != 2 or codes.dtype != torch.int8:
+        _refuse(f"{what}: codes are a matrix of int8, got {codes.dtype} {tuple(codes.shape)}")
     n, k = codes.shape
     width = -(-k // 16) * 16
     stride = codes.stride(0) if n > 1 else width
@@ -280,13 +287,16 @@ def ivfpq_q8_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torc
     a, a_stride = _code_rows(what, a_codes)
     b, b_stride = _code_rows(what, b_codes)
     (m, k), n = a_codes.shape, b_codes.shape[0]
-    _need(b_codes.shape[1] == k, f"{what}: rows of {k} and {b_codes.shape[1]} codes")
-    sa, sb = _plain(what, a_scales, torch.float32, (m,)), _plain(what, b_scales, torch.float32, (n,))
-    bias = None if bias is None else _plain(what, bias, torch.float32, (n,))
+    if b_codes.shape[1] != k:
+        _refuse(f"{what}: rows of {k} and {b_codes.shape[1]} codes")
+    sa, sb = _plain(what, a_scales, torch.float32, m), _plain(what, b_scales, torch.float32, n)
+    bias = None if bias is None else _plain(what, bias, torch.float32, n)
     if out is None:
-        _need(out_dtype in VALUES_DTYPES, f"{what}: out_dtype {out_dtype}")
+        if out_dtype not in VALUES_DTYPES:
+            _refuse(f"{what}: out_dtype {out_dtype}")
         out = torch.empty((m, n), dtype=out_dtype, device="cuda")
-    _need(out.shape == (m, n) and out.dtype in VALUES_DTYPES and (n <= 1 or out.stride(1) == 1), f"{what}: out has another shape, type or layout")
+    if out.shape != (m, n) or out.dtype not in VALUES_DTYPES or not _rows_apart(out):
+        _refuse(f"{what}: out has another shape, type or layout")
     _check(lib().ivfpq_q8_matmul(_dp(a), a_stride, _dp(sa), m, _dp(b), b_stride, _dp(sb), n, k, _dp(bias), _dp(out),
                                  VALUES_DTYPES[out.dtype], out.stride(0), _stream()))
     return out
@@ -296,10 +306,11 @@ def ivfpq_neighbour_tokens(ids: torch.Tensor, dists: torch.Tensor, id_tokens: to
     """-> (tokens int32 [nq][k], log-probabilities fp32 [nq][k]) of search results; id_tokens [n_ids] int32 is the token of every id."""
     what = "ivfpq_neighbour_tokens"
     _on_device(what, ids, dists, id_tokens)
-    _need(ids.dim() == 2, f"{what}: ids are a matrix")
+    if ids.dim() != 2:
+        _refuse(f"{what}: ids are a matrix")
     nq, k = ids.shape
-    ids, dists = _plain(what, ids, torch.int64, (nq, k)), _plain(what, dists, torch.float32, (nq, k))
-    table = _plain(what, id_tokens, torch.int32, (id_tokens.numel(),))
+    ids, dists = _plain(what, ids, torch.int64, nq, k), _plain(what, dists, torch.float32, nq, k)
+    table = _plain(what, id_tokens, torch.int32, id_tokens.numel())
     tokens = torch.empty((nq, k), dtype=torch.int32, device="cuda")
     logprobs = torch.empty((nq, k), dtype=torch.float32, device="cuda")
     _check(lib().ivfpq_neighbour_tokens(_dp(ids), _dp(dists), nq, k, _dp(table), table.numel(), temperature, _dp(tokens), _dp(logprobs), _stream()))
@@ -314,7 +325,7 @@ def ivfpq_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] =
     _on_device(what, logits, targets, *(neighbours or ()))
     x = _value_rows(what, logits)
     n, vocab = x.shape
-    targets = None if targets is None else _plain(what, targets, torch.int32, (n,))
+    targets = None if targets is None else _plain(what, targets, torch.int32, n)
     near_tokens, near_logprobs = (None, None) if neighbours is None else _listed(what, *neighbours, n)
     k = 0 if near_tokens is None else near_tokens.shape[1]
     logprobs = None if targets is None else torch.empty(n, dtype=torch.float32, device="cuda")
@@ -336,9 +347,9 @@ def ivfpq_token_logprobs_backward(logits: torch.Tensor, targets: Optional[torch.
     _on_device(what, logits, targets, norms, entropy, grad_logprobs, grad_entropy)
     x = _value_rows(what, logits)
     n = x.shape[0]
-    row = lambda t, dtype=torch.float32: None if t is None else _plain(what, t, dtype, (n,))
+    row = lambda t, dtype=torch.float32: None if t is None else _plain(what, t, dtype, n)
     targets, entropy, by_logprob, by_entropy = row(targets, torch.int32), row(entropy), row(grad_logprobs), row(grad_entropy)
-    norms = _plain(what, norms, torch.float32, (n, 2))
+    norms = _plain(what, norms, torch.float32, n, 2)
     grad = _grad_like(what, x, out)
     _check(lib().ivfpq_token_logprobs_backward(*_logits(x), _dp(targets), temperature, _dp(norms), _dp(entropy), _dp(by_logprob),
                                                _dp(by_entropy), _dp(grad), grad.stride(0), _stream()))
@@ -370,8 +381,8 @@ def ivfpq_distill_topk_backward(logits: torch.Tensor, norms: torch.Tensor, teach
     x = _value_rows(what, logits)
     n = x.shape[0]
     tokens, values = _listed(what, teacher_tokens, teacher_logits, n)
-    norms = _plain(what, norms, torch.float32, (n, 2))
-    row_grads = None if row_grads is None else _plain(what, row_grads, torch.float32, (n,))
+    norms = _plain(what, norms, torch.float32, n, 2)
+    row_grads = None if row_grads is None else _plain(what, row_grads, torch.float32, n)
     grad = _grad_like(what, x, out)
     _check(lib().ivfpq_distill_topk_backward(*_logits(x), _dp(norms), _dp(tokens), _dp(values), tokens.shape[1], temperature, _dp(row_grads),
                                              _dp(grad), grad.stride(0), _stream()))
@@ -386,7 +397,7 @@ def ivfpq_distill_topk_step(logits: torch.Tensor, teacher_tokens: torch.Tensor, 
     x = _value_rows(what, logits)
     n, vocab = x.shape
     tokens, values = _listed(what, teacher_tokens, teacher_logits, n)
-    row_grads = None if row_grads is None else _plain(what, row_grads, torch.float32, (n,))
+    row_grads = None if row_grads is None else _plain(what, row_grads, torch.float32, n)
     loss = torch.empty(n, dtype=torch.float32, device="cuda")
     grad = _grad_like(what, x, out)
     need = lib().ivfpq_distill_topk_workspace_bytes(n, vocab)

@@ -362,15 +362,32 @@ __device__ inline bool teacher_uses(const Listed& l, long long row, int j, int v
     const int token = l.tokens[row * l.k + j];
     return token >= 0 && token < vocab && l.values[row * l.k + j] != -INFINITY;
 }
+template <int THREADS>
 __device__ inline Teacher teacher_of(const Listed& l, long long row, int vocab, float scale, float* scratch) {
     float most = -INFINITY;
-    for (int j = threadIdx.x; j < l.k; j += kRowThreads)
+    for (int j = threadIdx.x; j < l.k; j += THREADS)
         if (teacher_uses(l, row, j, vocab)) most = fmaxf(most, l.values[row * l.k + j]);
-    most = block_max<kRowThreads>(most, scratch);
+    most = block_max<THREADS>(most, scratch);
     float total = 0.f;
-    for (int j = threadIdx.x; j < l.k; j += kRowThreads)
+    for (int j = threadIdx.x; j < l.k; j += THREADS)
         if (teacher_uses(l, row, j, vocab)) total += exp2_fast((l.values[row * l.k + j] - most) * scale);
-    return Teacher{most, block_sum<kRowThreads>(total, scratch)};
+    return Teacher{most, block_sum<THREADS>(total, scratch)};
+}
+
+// The row's loss, in every thread; x_of(j): the logit of entry j's token.
+template <int THREADS, class XOf>
+__device__ inline float loss_of(const RowsIn& in, const Listed& l, const Teacher& teacher, long long row, float m, float log_s, bool none, float* scratch, XOf&& x_of) {
+    const float log_total = logf(teacher.total);
+    float loss = 0.f;
+    for (int j = threadIdx.x; j < l.k; j += THREADS) {
+        if (!teacher_uses(l, row, j, in.vocab)) continue;
+        const float at = (l.values[row * l.k + j] - teacher.most) * in.scale;
+        const float share = exp2_fast(at) / teacher.total;
+        if (share == 0.f) continue;
+        const float logp = none ? -INFINITY : (x_of(j) - m) / in.temperature - log_s;
+        loss += share * (__builtin_fmaf(at, kLn2, -log_total) - logp);
+    }
+    return block_sum<THREADS>(loss, scratch) * in.temperature * in.temperature;
 }
 
 template <class T>
@@ -378,21 +395,11 @@ __device__ inline void finish_distill(const RowsIn& in, const DistillOut& out, l
     const T* x = reinterpret_cast<const T*>(in.data) + row * in.stride;
     const bool none = sum.s == 0.f;
     const float log_s = logf(sum.s);
-    const Teacher teacher = teacher_of(out.teacher, row, in.vocab, in.scale, scratch);
-    const float log_total = logf(teacher.total);
-    float loss = 0.f;
-    for (int j = threadIdx.x; j < out.teacher.k; j += kRowThreads) {
-        if (!teacher_uses(out.teacher, row, j, in.vocab)) continue;
-        const float at = (out.teacher.values[row * out.teacher.k + j] - teacher.most) * in.scale;
-        const float share = exp2_fast(at) / teacher.total;
-        if (share == 0.f) continue;
-        const float v = (float)x[out.teacher.tokens[row * out.teacher.k + j]];
-        const float logp = none ? -INFINITY : (v - sum.m) / in.temperature - log_s;
-        loss += share * (__builtin_fmaf(at, kLn2, -log_total) - logp);
-    }
-    loss = block_sum<kRowThreads>(loss, scratch);
+    const Teacher teacher = teacher_of<kRowThreads>(out.teacher, row, in.vocab, in.scale, scratch);
+    const float loss = loss_of<kRowThreads>(in, out.teacher, teacher, row, sum.m, log_s, none, scratch,
+                                            [&](int j) { return (float)x[out.teacher.tokens[row * out.teacher.k + j]]; });
     if (threadIdx.x == 0) {
-        out.loss[row] = loss * in.temperature * in.temperature;
+        out.loss[row] = loss;
         write_norms(out.norms, row, sum.m, log_s, none);
     }
 }
@@ -723,12 +730,55 @@ struct DistillGrad {
     const float* row_grads;
 };
 
+template <int THREADS>
 struct GradShared {
-    float scratch[kRowWaves];
-    int token[IVFPQ_MAX_LISTED];
+    float scratch[THREADS / 64];
+    alignas(16) int token[IVFPQ_MAX_LISTED];
     float share[IVFPQ_MAX_LISTED];
     float x[IVFPQ_MAX_LISTED];
 };
+
+// The listed tokens in [token0, token1) with their logits and what they add to the gradient, -w P_j; -1 for unused entries and up
+// to a multiple of 16 behind them.  Before anything is written: the gradient may lie over the logits.
+template <class T, int THREADS>
+__device__ inline void stage_listed(const Listed& l, const RowChunks<T>& row, long long r, int vocab, const Teacher& teacher, float scale, float w, int token0,
+                                    int token1, GradShared<THREADS>& lds) {
+    for (int j = threadIdx.x; j < (l.k + 15) / 16 * 16; j += THREADS) {
+        const bool used = j < l.k && teacher_uses(l, r, j, vocab);
+        const int token = used ? l.tokens[r * l.k + j] : -1;
+        lds.token[j] = token;
+        if (!used) continue;
+        lds.share[j] = -w * exp2_fast((l.values[r * l.k + j] - teacher.most) * scale) / teacher.total;
+        lds.x[j] = token >= token0 && token < token1 ? row.value(token) : 0.f;
+    }
+}
+
+// The elements of the listed tokens, once more and whole, behind a barrier after the others.  Entries of one token add up, in
+// their order, at the first of them.
+template <class T, int THREADS, class Dense>
+__device__ inline void write_listed(int k, int token0, int token1, const GradShared<THREADS>& lds, T* grad, Dense&& dense) {
+    for (int j = threadIdx.x; j < k; j += THREADS) {
+        const int token = lds.token[j];
+        if (token < token0 || token >= token1) continue;
+        int same = 0;
+        for (int i = 0; i < k; i += 16) {
+            int4 some[4];
+#pragma unroll
+            for (int o = 0; o < 4; ++o) some[o] = *reinterpret_cast<const int4*>(&lds.token[i + 4 * o]);
+#pragma unroll
+            for (int o = 0; o < 4; ++o) same += (some[o].x == token) + (some[o].y == token) + (some[o].z == token) + (some[o].w == token);
+        }
+        float share = lds.share[j];
+        bool first = true;
+        if (same > 1)
+            for (int i = 0; i < k; ++i)
+                if (i != j && lds.token[i] == token) {
+                    first &= i > j;
+                    share += lds.share[i];
+                }
+        if (first) grad[token] = (T)(dense(lds.x[j]) + share);
+    }
+}
 
 // grad_v = p_v (a + b t_v), t_v = log2 p_v, plus a term at a few listed tokens; a row without a distribution has zeros.
 // One workgroup: the chunks [split * chunks, ...) of a row.  The listed tokens' logits are read before anything is
@@ -737,7 +787,7 @@ template <class T, bool BY_ENTROPY, class How>
 __global__ __launch_bounds__(kRowThreads) void row_gradient_kernel(RowsIn in, GradIn g, How how) {
     constexpr int VEC = Chunk<T>::VEC;
     constexpr bool POLICY = std::is_same<How, PolicyGrad>::value;
-    __shared__ GradShared lds;
+    __shared__ GradShared<kRowThreads> lds;
     const int tid = threadIdx.x;
     const long long r = blockIdx.x / (unsigned)g.splits;
     const int part = blockIdx.x % (unsigned)g.splits;
@@ -762,22 +812,17 @@ __global__ __launch_bounds__(kRowThreads) void row_gradient_kernel(RowsIn in, Gr
             b = -gh * kLn2;
         }
         k = wanted && how.by_logprob ? 1 : 0;
+        if (tid > 0 && tid < 16) lds.token[tid] = -1;
         if (tid == 0 && k) {
             lds.token[0] = target;
             lds.share[0] = gl;
             lds.x[0] = target >= token0 && target < token1 ? row.value(target) : 0.f;
         }
     } else {
-        const Teacher teacher = teacher_of(how.teacher, r, in.vocab, in.scale, lds.scratch);
+        const Teacher teacher = teacher_of<kRowThreads>(how.teacher, r, in.vocab, in.scale, lds.scratch);
         const float w = in.temperature * (how.row_grads ? how.row_grads[r] : 1.f);
         k = how.teacher.k;
-        for (int j = tid; j < k; j += kRowThreads) {
-            const bool used = teacher_uses(how.teacher, r, j, in.vocab);
-            const int token = used ? how.teacher.tokens[r * k + j] : -1;
-            lds.token[j] = token;
-            lds.share[j] = used ? -w * exp2_fast((how.teacher.values[r * k + j] - teacher.most) * in.scale) / teacher.total : 0.f;
-            lds.x[j] = used && token >= token0 && token < token1 ? row.value(token) : 0.f;
-        }
+        stage_listed(how.teacher, row, r, in.vocab, teacher, in.scale, w, token0, token1, lds);
         a = teacher.total == 0.f ? 0.f : w;                // a NaN among the values stays one
     }
     __syncthreads();
@@ -807,24 +852,99 @@ __global__ __launch_bounds__(kRowThreads) void row_gradient_kernel(RowsIn in, Gr
     }
     if (none) return;
     __syncthreads();
-    for (int j = tid; j < k; j += kRowThreads) {
-        const int token = lds.token[j];
-        if (token < token0 || token >= token1) continue;
-        float share = lds.share[j];
-        bool first = true;
-        if constexpr (!POLICY)                             // entries of one token add up, in their order, at the first of them
-            for (int i = 0; i < k; ++i)
-                if (i != j && lds.token[i] == token) {
-                    first &= i > j;
-                    share += lds.share[i];
-                }
-        if (first) grad[token] = (T)(dense(lds.x[j]) + share);
+    write_listed(k, token0, token1, lds, grad, dense);
+}
+
+// Loss and gradient in one pass, for rows that fit the registers of a workgroup (HELD 16-byte chunks a thread): every
+// logit is read once and every element of the gradient written once.
+template <class T, int THREADS, int HELD>
+__global__ __launch_bounds__(THREADS) void distill_step_kernel(RowsIn in, DistillGrad how, float* __restrict__ loss, void* grads, long long grad_stride) {
+    constexpr int VEC = Chunk<T>::VEC;
+    __shared__ GradShared<THREADS> lds;
+    const int tid = threadIdx.x;
+    const long long r = blockIdx.x;
+    const RowChunks<T> row(in.data, r, in.stride, in.vocab), to(grads, r, grad_stride, in.vocab);
+    T* grad = const_cast<T*>(to.row);
+    const int begin = row.first_whole(), end = row.end_whole();
+    const bool front = !row.whole(0), back = end > 0 && row.end % VEC;
+    const bool alike = to.lead == row.lead;                // chunks of both lie alike
+    Chunk<T> held[HELD], edge[1];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+        if (begin + i * THREADS < end) held[i].bits = row.base[min(begin + i * THREADS + tid, end - 1)];
+    const int edge_chunk = load_edges(row, front, back, edge);
+    const Teacher teacher = teacher_of<THREADS>(how.teacher, r, in.vocab, in.scale, lds.scratch);
+    const float w = in.temperature * (how.row_grads ? how.row_grads[r] : 1.f);
+    stage_listed(how.teacher, row, r, in.vocab, teacher, in.scale, w, 0, in.vocab, lds);
+
+    float most[1];
+    largest_of_chunks(edge, most);
+    float m = most[0];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+        if (begin + i * THREADS < end) {                   // a chunk that stands in for one behind the last changes no maximum
+            float x[VEC];
+            held[i].widen(x);
+#pragma unroll
+            for (int j = 0; j < VEC; j += 2) m = max3(m, x[j], x[j + 1]);
+        }
+    m = block_max<THREADS>(m, lds.scratch);                // and a barrier behind stage_listed
+    const float ref = m == -INFINITY ? 0.f : m;
+    float s = 0.f;
+    auto add = [&](Chunk<T>& k) {
+        float x[VEC];
+        k.forget_widened();
+        k.widen(x);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) s += exp2_fast((x[j] - ref) * in.scale);
+    };
+    if (front || back) add(edge[0]);
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+        if (begin + i * THREADS + tid < end) add(held[i]);
+    s = block_sum<THREADS>(s, lds.scratch);
+    const bool none = s == 0.f;
+    const float log_s = logf(s), log2_s = log_s * kLog2E;
+    if (s != s) m = s;                                     // a NaN that is no number's equal is no maximum either
+    const float a = teacher.total == 0.f ? 0.f : w;
+    auto dense = [&](float x) { return a * exp2_fast(__builtin_fmaf(x - m, in.scale, -log2_s)); };
+    const float row_loss = loss_of<THREADS>(in, how.teacher, teacher, r, m, log_s, none, lds.scratch, [&](int j) { return lds.x[j]; });
+    if (tid == 0) loss[r] = row_loss;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+        if (begin + i * THREADS + tid < end) {
+            float x[VEC];
+            held[i].forget_widened();
+            held[i].widen(x);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) x[j] = none ? 0.f : dense(x[j]);
+            const int c = begin + i * THREADS + tid;
+            if (alike) {
+                Chunk<T> y;
+                y.narrow(x);
+                const_cast<uint4*>(to.base)[c] = y.bits;
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) grad[c * VEC + j - row.lead] = (T)x[j];
+            }
+        }
+    if ((tid == 0 && front) || (tid == 1 && back)) {
+        float x[VEC];
+        edge[0].widen(x);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const int v = edge_chunk * VEC + j - row.lead;
+            if (v >= 0 && v < in.vocab) grad[v] = (T)(none ? 0.f : dense(x[j]));
+        }
     }
+    if (none) return;
+    __syncthreads();
+    write_listed(how.teacher.k, 0, in.vocab, lds, grad, dense);
 }
 
 // ---- launches
 
-constexpr int64_t kMostRows = 1 << 23;                      // a launch has fewer than 2^32 threads
+constexpr int64_t kMostRows = 1 << 21;                      // a launch has fewer than 2^32 threads
 constexpr float kLeastTemperature = 1e-6f, kMostTemperature = 1e6f;       // T^2 and log2(e) / T stay moderate
 
 // How a row is dealt to workgroups: enough of them to fill the GPU, at least a chunk for every thread, at most kMostSplits.
@@ -844,7 +964,7 @@ int check_rows(const char* what, const void* data, int32_t dtype, int64_t n, int
     if (!known_dtype(dtype)) return fail(IVFPQ_EINVAL, "%s: unknown dtype %d", what, dtype);
     if (n < 0 || vocab < 1) return fail(IVFPQ_EINVAL, "%s: bad shape (n=%lld vocab=%d)", what, (long long)n, vocab);
     if (vocab > (1 << 30)) return fail(IVFPQ_EUNSUPPORTED, "%s: vocab=%d (limit 2^30)", what, vocab);
-    if (n > kMostRows) return fail(IVFPQ_EUNSUPPORTED, "%s: n=%lld (limit 2^23 rows per call)", what, (long long)n);
+    if (n > kMostRows) return fail(IVFPQ_EUNSUPPORTED, "%s: n=%lld (limit 2^21 rows per call)", what, (long long)n);
     if (n > 1 && stride < vocab) return fail(IVFPQ_EINVAL, "%s: row stride %lld below vocab=%d", what, (long long)stride, vocab);
     if (!(temperature >= kLeastTemperature && temperature <= kMostTemperature))
         return fail(IVFPQ_EINVAL, "%s: temperature outside [%g, %g]", what, (double)kLeastTemperature, (double)kMostTemperature);
@@ -974,6 +1094,34 @@ int distill_gradient(const RowsIn& in, int32_t dtype, int64_t n, const Listed& t
     return with_value_type(dtype, [&](auto v) { return launch_gradient<decltype(v), false>(n, in, g, how, stream); });
 }
 
+// Rows in registers where they fit: one launch and one read of the logits instead of three and two (4,096 x 65,536 bf16: 266 against
+// 372 us).  A few long rows are better split between many workgroups.
+constexpr int kHeldChunks = 16;
+bool step_in_registers(int64_t n, int32_t vocab, int32_t dtype) {
+    const int64_t bytes = (int64_t)vocab * value_bytes(dtype);
+    return bytes <= (int64_t)16 * kHeldChunks * 1024 && (n >= 16 || bytes <= 65536);
+}
+
+template <class T, int THREADS, int HELD>
+int launch_step(int64_t n, const RowsIn& in, const DistillGrad& how, float* d_loss, void* d_grad, int64_t grad_stride, hipStream_t stream) {
+    hipLaunchKernelGGL((distill_step_kernel<T, THREADS, HELD>), dim3((unsigned)n), dim3(THREADS), 0, stream, in, how, d_loss, d_grad, (long long)grad_stride);
+    HIP_TRY(hipGetLastError());
+    return IVFPQ_OK;
+}
+
+int distill_step(const RowsIn& in, int32_t dtype, int64_t n, const Listed& teacher, const float* d_row_grads, float* d_loss, void* d_grad,
+                 int64_t grad_stride, hipStream_t stream) {
+    const DistillGrad how{teacher, d_row_grads};
+    const int64_t chunks = ((int64_t)in.vocab * value_bytes(dtype) + 15) / 16;
+    return with_value_type(dtype, [&](auto v) {
+        using T = decltype(v);
+        if (chunks <= 4 * 256) return launch_step<T, 256, 4>(n, in, how, d_loss, d_grad, grad_stride, stream);      // fewer registers: twice the rows at once
+        if (chunks <= kHeldChunks * 256) return launch_step<T, 256, kHeldChunks>(n, in, how, d_loss, d_grad, grad_stride, stream);
+        if (chunks <= kHeldChunks * 512) return launch_step<T, 512, kHeldChunks>(n, in, how, d_loss, d_grad, grad_stride, stream);
+        return launch_step<T, 1024, kHeldChunks>(n, in, how, d_loss, d_grad, grad_stride, stream);
+    });
+}
+
 size_t distill_scratch(int64_t n, int32_t vocab) {
     if (n < 1 || n > kMostRows) return 0;
     return align_up((size_t)n * 2 * sizeof(float)) + row_workspace(n, vocab, 0);      // norms of a step, then the split rows
@@ -1076,6 +1224,8 @@ int ivfpq_distill_topk_step(const void* d_logits, int32_t dtype, int64_t n, int3
         const RowsIn in = rows_in(d_logits, row_stride, vocab, temperature);
         const Listed teacher{d_teacher_tokens, d_teacher_logits, k};
         const hipStream_t stream = (hipStream_t)hip_stream;
+        if (step_in_registers(n, vocab, dtype))
+            return distill_step(in, dtype, n, teacher, d_row_grads, d_loss, d_grad, grad_stride, stream);
         if (int s = distill_forward(what, in, dtype, n, teacher, d_loss, norms, split, stream)) return s;
         return distill_gradient(in, dtype, n, teacher, d_row_grads, norms, d_grad, grad_stride, stream);
     });

@@ -39,7 +39,7 @@ QUANT = dict(rows=A, dtype=0, n=3, d=50, stride=50, codes=A, code_stride=64, sca
 
 ROWS = [
     (dict(dtype=3), "EINVAL", "dtype"), (dict(dtype=-1), "EINVAL", "dtype"), (dict(n=-1), "EINVAL", "shape"), (dict(vocab=0), "EINVAL", "shape"),
-    (dict(vocab=(1 << 30) + 1, stride=1 << 31), "EUNSUPPORTED", "vocab"), (dict(n=(1 << 23) + 1), "EUNSUPPORTED", "rows"), (dict(stride=99), "EINVAL", "stride"),
+    (dict(vocab=(1 << 30) + 1, stride=1 << 31), "EUNSUPPORTED", "vocab"), (dict(n=(1 << 21) + 1), "EUNSUPPORTED", "rows"), (dict(stride=99), "EINVAL", "stride"),
     (dict(logits=0), "EINVAL", "null"), (dict(logits=A + 2), "EINVAL", "aligned"), (dict(temperature=0.0), "EINVAL", "temperature"),
     (dict(temperature=-1.0), "EINVAL", "temperature"), (dict(temperature=math.nan), "EINVAL", "temperature"), (dict(temperature=math.inf), "EINVAL", "temperature"),
     (dict(temperature=1e-7), "EINVAL", "temperature"),
