@@ -1,7 +1,9 @@
 // Search results as a distribution over tokens: what ivfpq_neighbour_tokens does.
 //
 // With t_j = (d_min - d_j) log2(e) / T the weight of neighbour j is 2^t_j; the neighbours that share a token add up at the
-// first of them.  A query's neighbours are in the LDS and each is compared with all the others (k^2 comparisons a query).
+// first of them.  A query's tokens are in a hash table in the LDS, so the work goes with k.  A token's weights are taken about its
+// nearest neighbour and added as whole numbers of 2^-53 (the largest is 1, at most 1024 are added): exact to 2^-43 of the
+// sum, and the same in any order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -25,9 +27,9 @@ struct NeighboursIn {
 // One workgroup a query; K: room for neighbours.
 template <int THREADS, int K>
 __global__ __launch_bounds__(THREADS) void neighbour_tokens_kernel(NeighboursIn in, int* __restrict__ tokens, float* __restrict__ logprobs) {
-    constexpr int EACH = K / THREADS, WAVES = THREADS / 64;
-    __shared__ int token[K];
-    __shared__ float weight[K], power[K];
+    constexpr int EACH = K / THREADS, WAVES = THREADS / 64, SLOTS = 2 * K;      // at most half full
+    __shared__ unsigned long long sums[SLOTS];
+    __shared__ int keys[SLOTS], first_of[SLOTS], near_of[SLOTS];               // near_of: the bits of the smallest -t
     __shared__ float scratch[WAVES];
     __shared__ int firsts[EACH * WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = in.k;
@@ -46,51 +48,57 @@ __global__ __launch_bounds__(THREADS) void neighbour_tokens_kernel(NeighboursIn 
             if (id >= 0 && id < in.n_ids && fabsf(d) < INFINITY) {
                 mine[i] = in.id_tokens[id];
                 if (mine[i] >= 0) dist[i] = d;
+                else mine[i] = -1;
             }
         }
         nearest = fminf(nearest, dist[i]);
     }
-    nearest = -block_max<THREADS>(-nearest, scratch);
+    for (int i = tid; i < SLOTS; i += THREADS) {
+        keys[i] = -1;
+        first_of[i] = K;
+        near_of[i] = 0x7FFFFFFF;
+        sums[i] = 0;
+    }
+    nearest = -block_max<THREADS>(-nearest, scratch);      // and barriers behind the cleared table
     float total = 0.f;
+    float far[EACH];                                       // -t
+    int slot[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        const int j = i * THREADS + tid;
-        if (j >= k) continue;
-        const float t = mine[i] >= 0 ? (nearest - dist[i]) * in.scale : -INFINITY;
-        const float w = exp2_fast(t);
-        token[j] = mine[i];
-        power[j] = t;
-        weight[j] = w;
-        total += w;
+        far[i] = 0.f;
+        slot[i] = 0;
+        if (mine[i] < 0) continue;
+        far[i] = fabsf((nearest - dist[i]) * in.scale);
+        total += exp2_fast(-far[i]);
+        unsigned at = ((unsigned)mine[i] * 2654435761u) >> 16 & (SLOTS - 1);
+        for (;;) {                                         // ends: more slots than tokens
+            const int held = atomicCAS(&keys[at], -1, mine[i]);
+            if (held == -1 || held == mine[i]) break;
+            at = (at + 1) & (SLOTS - 1);
+        }
+        slot[i] = (int)at;
+        atomicMin(&first_of[at], i * THREADS + tid);
+        atomicMin(&near_of[at], __float_as_int(far[i]));   // numbers that are not negative: their bits have their order
     }
-    const float log_total = logf(block_sum<THREADS>(total, scratch));
+    const float log_total = logf(block_sum<THREADS>(total, scratch));      // and barriers behind the filled table
 
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (mine[i] >= 0) {
+            const float near = __int_as_float(near_of[slot[i]]);
+            if (near < INFINITY) atomicAdd(&sums[slot[i]], (unsigned long long)(exp2_fast(near - far[i]) * 0x1p53f));
+        }
+    __syncthreads();
     float logp[EACH];
     bool first[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        const int j = i * THREADS + tid;
-        first[i] = false;
-        if (j >= k || mine[i] < 0) continue;
-        bool lead = true;
-        float sum = 0.f;
-        for (int o = 0; o < k; ++o) {
-            const bool same = token[o] == mine[i];
-            sum += same ? weight[o] : 0.f;
-            lead &= !(same && o < j);
-        }
-        first[i] = lead;
-        if (!lead) continue;
-        float most = 0.f;
-        if (sum < 1e-30f) {                                // far neighbours only: about the nearest of them
-            most = -INFINITY;
-            for (int o = 0; o < k; ++o)
-                if (token[o] == mine[i]) most = fmaxf(most, power[o]);
-            sum = 0.f;
-            for (int o = 0; o < k; ++o)
-                if (token[o] == mine[i]) sum += exp2_fast(power[o] - most);
-        }
-        logp[i] = most == -INFINITY ? most : most * kLn2 + logf(sum) - log_total;       // -inf: over 10^38 temperatures away
+        first[i] = mine[i] >= 0 && first_of[slot[i]] == i * THREADS + tid;
+        logp[i] = 0.f;
+        if (!first[i]) continue;
+        const float near = __int_as_float(near_of[slot[i]]);
+        // -inf: over 10^38 temperatures away
+        logp[i] = near == INFINITY ? -INFINITY : logf((float)sums[slot[i]] * 0x1p-53f) - near * kLn2 - log_total;
     }
     // places: the distinct tokens before this one
 #pragma unroll
