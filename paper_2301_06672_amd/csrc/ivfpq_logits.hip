@@ -251,9 +251,28 @@ __device__ inline void write_norms(float* norms, long long row, float m, float l
     norms[2 * row + 1] = none ? -INFINITY : log_s;
 }
 
+// A row's target and its logit; read before the row, so that their latency is not at the end of it.
+struct Target {
+    int token = -1;                   // as given
+    bool inside = false;
+    float x = 0.f;
+};
+template <class T>
+__device__ inline Target target_of(const RowsIn& in, const ScoreOut& out, long long row) {
+    Target t;
+    if (!out.targets) return t;
+    t.token = out.targets[row];
+    t.inside = t.token >= 0 && t.token < in.vocab;
+    if (t.inside) t.x = (float)reinterpret_cast<const T*>(in.data)[row * in.stride + t.token];
+    return t;
+}
+template <class T>
+__device__ inline Target target_of(const RowsIn&, const DistillOut&, long long) { return Target{}; }
+
 // All threads of a workgroup, on the statistics of one row; kept: its `n_kept` largest keys (TOP).
 template <class T, bool TOP>
-__device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long long row, RowSum sum, int n_kept, Selection* sel, MixShared& mix) {
+__device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long long row, const Target& target, RowSum sum, int n_kept, Selection* sel,
+                                    MixShared& mix) {
     const int tid = threadIdx.x;
     const T* x = reinterpret_cast<const T*>(in.data) + row * in.stride;
     const bool none = sum.s == 0.f;                        // no logit above -inf (a largest one would have added 1)
@@ -261,13 +280,11 @@ __device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long 
     // log p of a logit
     auto model_logp = [&](float v) { return none ? -INFINITY : (v - sum.m) / in.temperature - log_s; };
     const float entropy = none ? 0.f : log_s - kLn2 * (sum.u / sum.s);
-    const int target = out.targets && tid == 0 ? out.targets[row] : -1;
-    const bool wanted = target >= 0 && target < in.vocab;
     if (tid == 0) write_norms(out.norms, row, sum.m, log_s, none);
 
     if (out.near.k == 0) {
         if (tid == 0) {
-            if (out.targets) out.logprobs[row] = wanted ? model_logp((float)x[target]) : 0.f;
+            if (out.targets) out.logprobs[row] = target.inside ? model_logp(target.x) : 0.f;
             if (out.entropy) out.entropy[row] = entropy;
         }
         if constexpr (TOP)
@@ -305,12 +322,9 @@ __device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long 
         if (mixed > kLeastPower || mixed != mixed) change -= (double)expf(mixed) * (double)mixed;
     }
     change = block_sum<kRowThreads>(change, mix.sums);     // and a barrier behind mix.hit, mix.logp
-    if (out.targets) {
-        const int t = out.targets[row];
-        if (t >= 0)
-            for (int j = tid; j < k; j += kRowThreads)
-                if (mix.token[j] == t) mix.hit = mix.logp[j];
-    }
+    if (target.inside)
+        for (int j = tid; j < k; j += kRowThreads)
+            if (mix.token[j] == target.token) mix.hit = mix.logp[j];
     __syncthreads();
     if (tid == 0) {
         if (out.entropy) {
@@ -320,7 +334,7 @@ __device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long 
         }
         if (out.targets) {
             const bool listed = mix.hit > -INFINITY || mix.hit != mix.hit;
-            out.logprobs[row] = !wanted ? 0.f : listed ? mix.hit : log_model + model_logp((float)x[target]);
+            out.logprobs[row] = !target.inside ? 0.f : listed ? mix.hit : log_model + model_logp(target.x);
         }
     }
     if constexpr (TOP) {
@@ -407,7 +421,7 @@ __device__ inline void finish_distill(const RowsIn& in, const DistillOut& out, l
 // ---- the pass over the logits
 
 // 16-byte chunks that a thread holds at once
-constexpr int kRowChunks = 4;
+constexpr int kRowChunks = 2;
 
 // Whole chunks c0, c0 + kRowThreads, ... of a row for a thread's place; from `end` on the last one again.  No branch, so that the
 // loads of the next tile stay in flight while this one is added up.
@@ -506,8 +520,21 @@ struct RowShared {
     float scratch[kRowWaves];
 };
 template <RowMode MODE> struct RowLds { RowShared rows; MixShared mix; };
-template <> struct RowLds<RowMode::kScoreTop> { RowShared rows; MixShared mix; Selection sel; };
+template <> struct RowLds<RowMode::kScoreTop> { RowShared rows; Selection sel; };
 template <> struct RowLds<RowMode::kDistill> { RowShared rows; };
+
+// Where a mixture's numbers are: with a selection in the back of its candidates, of which the last merge uses 2 kMostTop and
+// what fills up a step of counting.
+template <RowMode MODE>
+__device__ inline MixShared& mix_of(RowLds<MODE>& lds) {
+    if constexpr (MODE == RowMode::kScoreTop) {
+        constexpr int kFront = 3 * kMostTop;
+        static_assert(sizeof(MixShared) <= sizeof(lds.sel.found) - kFront * sizeof(uint64_t), "room for both");
+        return *reinterpret_cast<MixShared*>(lds.sel.found + kFront);
+    } else {
+        return lds.mix;
+    }
+}
 
 struct RowSplit {
     int splits, chunks;               // workgroups a row, chunks of each
@@ -527,9 +554,9 @@ __device__ inline RowSum block_join(RowSum sum, float scale, RowShared& lds) {
 }
 
 template <class T, RowMode MODE, class Out>
-__device__ inline void finish_row(const RowsIn& in, const Out& out, long long row, RowSum sum, int n_kept, RowLds<MODE>& lds) {
-    if constexpr (MODE == RowMode::kScoreTop) finish_score<T, true>(in, out, row, sum, n_kept, &lds.sel, lds.mix);
-    else if constexpr (MODE == RowMode::kScore) finish_score<T, false>(in, out, row, sum, 0, nullptr, lds.mix);
+__device__ inline void finish_row(const RowsIn& in, const Out& out, long long row, const Target& target, RowSum sum, int n_kept, RowLds<MODE>& lds) {
+    if constexpr (MODE == RowMode::kScoreTop) finish_score<T, true>(in, out, row, target, sum, n_kept, &lds.sel, mix_of<MODE>(lds));
+    else if constexpr (MODE == RowMode::kScore) finish_score<T, false>(in, out, row, target, sum, 0, nullptr, mix_of<MODE>(lds));
     else finish_distill<T>(in, out, row, sum, lds.rows.scratch);
 }
 
@@ -580,7 +607,7 @@ __device__ inline int select_step_by_step(const RowChunks<T>& row, int begin, in
 // those is collected from the next tiles without a barrier, merged after 4, 16, ... tiles (a bound from N tiles lets about as
 // many of the next N pass as are wanted).
 template <class T, RowMode MODE, class Out>
-__global__ __launch_bounds__(kRowThreads, 5) void row_statistics_kernel(RowsIn in, RowSplit split, Out out) {
+__global__ __launch_bounds__(kRowThreads, 6) void row_statistics_kernel(RowsIn in, RowSplit split, Out out) {
     constexpr int VEC = Chunk<T>::VEC;
     constexpr bool TOP = MODE == RowMode::kScoreTop, ENTROPY = MODE != RowMode::kDistill;
     __shared__ RowLds<MODE> lds;
@@ -590,6 +617,7 @@ __global__ __launch_bounds__(kRowThreads, 5) void row_statistics_kernel(RowsIn i
     const int begin = row.first_whole() + part * split.chunks;
     const int end = min(begin + split.chunks, row.end_whole());
     const bool last = part + 1 == split.splits;
+    const Target target = split.splits == 1 ? target_of<T>(in, out, r) : Target{};
     const bool front = part == 0 && !row.whole(0), back = last && row.end_whole() > 0 && row.end % VEC;
     RowSum sum;
     uint64_t bound = 0;
@@ -657,7 +685,7 @@ __global__ __launch_bounds__(kRowThreads, 5) void row_statistics_kernel(RowsIn i
     sum = block_join(sum, in.scale, lds.rows);
     if (split.splits == 1) {
         __syncthreads();
-        finish_row<T, MODE>(in, out, r, sum, n_kept, lds);
+        finish_row<T, MODE>(in, out, r, target, sum, n_kept, lds);
         return;
     }
     const long long at = r * split.splits + part;
@@ -671,6 +699,7 @@ template <class T, RowMode MODE, class Out>
 __global__ __launch_bounds__(kRowThreads) void row_join_kernel(RowsIn in, RowSplit split, Out out) {
     __shared__ RowLds<MODE> lds;
     const long long r = blockIdx.x;
+    const Target target = target_of<T>(in, out, r);
     RowSum sum;
     if ((int)threadIdx.x < split.splits) sum = RowSum(split.partials[r * split.splits + threadIdx.x]);
     sum = block_join(sum, in.scale, lds.rows);
@@ -709,7 +738,7 @@ __global__ __launch_bounds__(kRowThreads) void row_join_kernel(RowsIn in, RowSpl
         });
     }
     __syncthreads();
-    finish_row<T, MODE>(in, out, r, sum, n_kept, lds);
+    finish_row<T, MODE>(in, out, r, target, sum, n_kept, lds);
 }
 
 // ---- gradients
