@@ -644,7 +644,9 @@ __global__ __launch_bounds__(kRowThreads, 6) void row_statistics_kernel(RowsIn i
         if (threadIdx.x == 0) lds.sel.n_found = 0;
         __syncthreads();
     }
-    Chunk<T> now[kRowChunks], next[kRowChunks];
+    Chunk<T> now[kRowChunks], next[kRowChunks], edge[1];
+    int edge_token = 0;
+    if (front || back) edge_token = load_edges(row, front, back, edge) * VEC - row.lead;       // ahead, as the tiles are
     if (begin < end) load_tile(row, begin, end, now);
     for (int c0 = begin; c0 < end; c0 += kRowChunks * kRowThreads) {
         const int c1 = c0 + kRowChunks * kRowThreads;
@@ -667,11 +669,9 @@ __global__ __launch_bounds__(kRowThreads, 6) void row_statistics_kernel(RowsIn i
         for (int i = 0; i < kRowChunks; ++i) now[i] = next[i];
     }
     if (front || back) {
-        Chunk<T> k[1];
         float most[1];
-        const int first = load_edges(row, front, back, k) * VEC - row.lead;
-        add_tile<T, ENTROPY>(k, in.scale, sum, most);
-        if (TOP && !many) scan_tile(k, most, first, bound, collect);
+        add_tile<T, ENTROPY>(edge, in.scale, sum, most);
+        if (TOP && !many) scan_tile(edge, most, edge_token, bound, collect);
     }
     if constexpr (TOP) {
         if (!many) merge();
@@ -976,12 +976,13 @@ __global__ __launch_bounds__(THREADS) void distill_step_kernel(RowsIn in, Distil
 constexpr int64_t kMostRows = 1 << 21;                      // a launch has fewer than 2^32 threads
 constexpr float kLeastTemperature = 1e-6f, kMostTemperature = 1e6f;       // T^2 and log2(e) / T stay moderate
 
-// How a row is dealt to workgroups: enough of them to fill the GPU, at least a chunk for every thread, at most kMostSplits.
+// How a row is dealt to workgroups: as many as run at once (six on each of 256 CUs; a few more would take as long as that many
+// again), at least a chunk for every thread, at most most_splits.
 RowSplit split_rows(int64_t n, int32_t vocab, int vec, int most_splits) {
-    constexpr int64_t kFill = 1024;                        // four workgroups on each of 256 CUs
+    constexpr int64_t kAtOnce = 6 * 256;
     const int64_t chunks = ((int64_t)vocab + vec - 1) / vec + 1;      // of a row at the worst alignment
     const int64_t useful = (chunks + kRowThreads - 1) / kRowThreads;
-    int64_t splits = std::min<int64_t>({(kFill + n - 1) / n, useful, most_splits});
+    const int64_t splits = std::min<int64_t>({std::max<int64_t>(kAtOnce / n, 1), useful, most_splits});
     RowSplit s{};
     s.chunks = (int)((chunks + splits - 1) / splits);
     s.chunks = (s.chunks + kRowThreads - 1) / kRowThreads * kRowThreads;
