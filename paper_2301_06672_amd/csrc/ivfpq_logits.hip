@@ -428,7 +428,7 @@ constexpr int kRowChunks = 2;
 template <class T>
 __device__ inline void load_tile(const RowChunks<T>& row, int c0, int end, Chunk<T> (&k)[kRowChunks]) {
 #pragma unroll
-    for (int i = 0; i < kRowChunks; ++i) k[i].bits = row.base[min(c0 + i * kRowThreads + (int)threadIdx.x, end - 1)];
+    for (int i = 0; i < kRowChunks; ++i) k[i].bits = row.base[(uint32_t)min(c0 + i * kRowThreads + (int)threadIdx.x, end - 1)];
 }
 
 template <class T>
@@ -470,28 +470,32 @@ __device__ inline void largest_of_chunks(const Chunk<T> (&k)[N], float (&most)[N
     }
 }
 
-// Adds the chunks to the sums about the thread's own maximum; leaves the maximum of every chunk.
+// Adds the chunks to a thread's sums; leaves the maximum of every chunk, and of all so far in `largest`.  The reference follows the
+// maximum only when that is over 2^kSlack of it: most tiles raise some lane's maximum by a little, and a raise costs as
+// much as an element.  The sums' parts stay within 2^kSlack of their place, so nothing is lost.
+constexpr float kSlack = 4.f;
 template <class T, bool ENTROPY, int N>
-__device__ inline void add_tile(Chunk<T> (&k)[N], float scale, RowSum& sum, float (&most)[N]) {
+__device__ inline void add_tile(Chunk<T> (&k)[N], float scale, RowSum& sum, float& largest, float (&most)[N]) {
     constexpr int VEC = Chunk<T>::VEC;
-    largest_of_chunks(k, most);
-    float top = sum.m;
-#pragma unroll
-    for (int i = 0; i < N; ++i) top = fmaxf(top, most[i]);
-    if (top > sum.m) sum.raise(top, scale);
-    const float ref = sum.m == -INFINITY ? 0.f : sum.m;     // nothing but -inf so far: t = -inf, not a NaN
+    float x[N][VEC];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        float x[VEC];
-        k[i].forget_widened();
-        k[i].widen(x);
+        k[i].widen(x[i]);
+        most[i] = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < VEC; j += 2) most[i] = max3(most[i], x[i][j], x[i][j + 1]);
+        largest = fmaxf(largest, most[i]);
+    }
+    if ((largest - sum.m) * scale > kSlack) sum.raise(largest, scale);
+    const float ref = sum.m == -INFINITY ? 0.f : sum.m;     // nothing but -inf so far: t = -inf, not a NaN
+#pragma unroll
+    for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            const float t = (x[j] - ref) * scale, e = exp2_fast(t);
+            const float t = (x[i][j] - ref) * scale, e = exp2_fast(t);
             sum.s += e;
             if constexpr (ENTROPY) sum.u = __builtin_fmaf(fmaxf(t, kLeastPower), e, sum.u);
         }
-    }
 }
 
 // The largest key of a thread's chunks, 0 if they hold nothing above -inf.
@@ -620,6 +624,7 @@ __global__ __launch_bounds__(kRowThreads, 6) void row_statistics_kernel(RowsIn i
     const Target target = split.splits == 1 ? target_of<T>(in, out, r) : Target{};
     const bool front = part == 0 && !row.whole(0), back = last && row.end_whole() > 0 && row.end % VEC;
     RowSum sum;
+    float largest = -INFINITY;
     uint64_t bound = 0;
     int n_kept = 0, want = 0, tiles = 0, merge_at = 1;
     bool many = false;                                     // more candidates than there is room for
@@ -653,7 +658,7 @@ __global__ __launch_bounds__(kRowThreads, 6) void row_statistics_kernel(RowsIn i
         load_tile(row, c1, end, next);
         cut_tile(c0, end, now);
         float most[kRowChunks];
-        add_tile<T, ENTROPY>(now, in.scale, sum, most);
+        add_tile<T, ENTROPY>(now, in.scale, sum, largest, most);
         if constexpr (TOP) {
             const int first = (c0 + (int)threadIdx.x) * VEC - row.lead;
             if (c0 == begin) bound = bound_of_best(lds.sel, best_of_tile(now, most, first), want);
@@ -670,7 +675,7 @@ __global__ __launch_bounds__(kRowThreads, 6) void row_statistics_kernel(RowsIn i
     }
     if (front || back) {
         float most[1];
-        add_tile<T, ENTROPY>(edge, in.scale, sum, most);
+        add_tile<T, ENTROPY>(edge, in.scale, sum, largest, most);
         if (TOP && !many) scan_tile(edge, most, edge_token, bound, collect);
     }
     if constexpr (TOP) {
@@ -682,6 +687,7 @@ __global__ __launch_bounds__(kRowThreads, 6) void row_statistics_kernel(RowsIn i
             n_kept = select_step_by_step(row, part == 0 ? 0 : min(begin, end), last ? row.count() : end, want, lds.sel);
         }
     }
+    if (largest > sum.m) sum.raise(largest, in.scale);
     sum = block_join(sum, in.scale, lds.rows);
     if (split.splits == 1) {
         __syncthreads();
