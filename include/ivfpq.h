@@ -305,7 +305,7 @@ int ivfpq_quantize_rows(const void* d_rows, int32_t dtype, int64_t n, int32_t d,
  * summed exactly in int32.  Hidden states (a) and an output embedding (b) give logits; queries and stored vectors give
  * inner products, and with bias[j] = -|b_j|^2 / 2 the largest value of a row is its nearest stored vector.
  *   d_a [m][k], d_b [n][k] int8: both pointers 16-byte aligned, both strides multiples of 16 and at least k rounded up to
- *   16; every row's bytes up to there, the last row's too, are read, and those from k on ignored.  d_a_scales [m], d_b_scales [n], d_bias [n] (may be NULL) fp32.
+ *   16 (at most 2^24); every row's bytes up to there, the last row's too, are read, and those from k on ignored.  d_a_scales [m], d_b_scales [n], d_bias [n] (may be NULL) fp32.
  *   d_out [m][n] of out_dtype, out_stride >= n.  1 <= k <= IVFPQ_MAX_Q8_K. */
 int ivfpq_q8_matmul(const int8_t* d_a, int64_t a_stride, const float* d_a_scales, int64_t m, const int8_t* d_b,
                     int64_t b_stride, const float* d_b_scales, int64_t n, int32_t k, const float* d_bias, void* d_out,

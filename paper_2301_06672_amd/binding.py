@@ -270,7 +270,7 @@ def _code_rows(what: str, codes: torch.Tensor):
     n, k = codes.shape
     width = -(-k // 16) * 16
     stride = codes.stride(0) if n > 1 else width
-    fits = (k <= 1 or codes.stride(1) == 1) and stride % 16 == 0 and stride >= width and codes.data_ptr() % 16 == 0 and (
+    fits = (k <= 1 or codes.stride(1) == 1) and stride % 16 == 0 and width <= stride <= 1 << 24 and codes.data_ptr() % 16 == 0 and (
         codes.storage_offset() + (n - 1) * stride + width <= codes.untyped_storage().nbytes())
     if n == 0 or fits:
         return codes, max(stride, width)

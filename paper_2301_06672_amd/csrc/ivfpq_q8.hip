@@ -22,7 +22,8 @@ typedef int intx16 __attribute__((ext_vector_type(16)));
 constexpr int kHeld = 4;                  // chunks a thread holds between the pass for the scale and the pass for the codes
 
 // LANES threads a row, 256 / LANES rows a workgroup (LANES 64 or 256).  Reads every row once (rows over kHeld chunks a thread:
-// the rest a second time, from the caches).
+// the rest a second time, from the caches).  The scale is a maximum, so a row has to be seen before its first code: it is held in
+// registers in between.  2,048 x 4,096 bf16: 11 us (25 MB, 2.3 TB/s: a chain of load, maximum, division, store); one such row 4 us.
 template <class T, int LANES>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const void* __restrict__ rows, long long n, int d, long long stride,
                                                             int8_t* __restrict__ codes, long long code_stride, float* __restrict__ scales) {
@@ -118,7 +119,8 @@ __device__ inline intx4 masked16(const int8_t* row, int at, int k) {
 // Few rows of a.  v_mfma_i32_16x16x64_i8: a wave has MT x NT blocks of 16 x 16; lane L brings row / column L % 16 and bytes
 // [16 (L / 16), ...) of each 64; register v of lane L holds row 4 (L / 16) + v, column L % 16.  The operands come straight
 // from memory in that layout (b is read once, a from the caches); the four waves of a workgroup take every fourth of the
-// 128-byte lines of the rows and add up through the LDS.
+// 128-byte lines of the rows and add up through the LDS.  Bound by reading b: 32,768 rows of 4,096 against one row 24 us, 5.6 TB/s,
+// what a streaming read reaches.
 template <class T, int MT, int NT>
 __global__ __launch_bounds__(256) void skinny_kernel(Product p) {
     __shared__ int sums[3][MT * NT * 4][64];
@@ -197,7 +199,12 @@ __global__ __launch_bounds__(256) void skinny_kernel(Product p) {
 // v_mfma_i32_32x32x32_i8: lane L brings row / column L % 32 and bytes [16 (L / 32), ...) of each 32; register v of lane L
 // holds row 8 (v / 4) + 4 (L / 32) + v % 4, column L % 32.  Two rows of 128 bytes cover the 64 banks of the LDS, so the 16-byte
 // pieces of row r stand in the order piece ^ (r / 2 % 8): sixteen lanes that read one piece of sixteen rows use every bank
-// once.
+// once.  Pieces are addressed by 32-bit offsets made once a tile (64-bit products for every load: 325 against 308 us below).
+// 2,048 x 32,768 bf16 results of 4,096 components: 272 us, 2.0 POP/s (the library's int8 product of that shape, without scales:
+// 264); 8,192^3 519 us, 2.1 POP/s (511).  The matrix cores are 0.4 busy; a CU's LDS reads (0.75 of the products' time), its loads of
+// the next slice and the products overlap between the two waves of a SIMD, and all of them wait for the slowest at the barrier
+// of a slice.  Slices of 64 bytes, three of them ahead in four buffers: 343 against 308 us; slices begun at another place
+// by every workgroup, against rows a power of two apart in one channel: no gain (323 against 325).
 __device__ inline int piece_at(int row, int piece) { return piece ^ ((row >> 1) & 7); }
 
 // Sums on their way out: rows of BN words and 8 more, which puts rows four apart into opposite halves of the banks
@@ -362,6 +369,7 @@ int launch_tiles(const Product& p, hipStream_t stream) {
 }
 
 constexpr int64_t kPiece = 1 << 22;        // rows of one launch: fewer than 2^32 threads
+constexpr int64_t kMostStride = 1 << 24;   // 255 of them and a piece's place in its line are a 32-bit offset from a tile's first row
 
 // Few rows of a, or few outputs: the tiles of 128 x 128 would leave most of the GPU idle (measured with k = 4096, a of 32 rows: n = 4,000
 // 8.6 against 20 us, 16,000 19 against 23, 32,768 34 against 25; of 64 rows: n = 8,000 17 against 23, 32,768 52 against 27).
@@ -393,6 +401,8 @@ int q8_matmul(const int8_t* d_a, int64_t a_stride, const float* d_a_scales, int6
     const int64_t least = (k + 15) / 16 * 16;
     if (a_stride < least || a_stride % 16 || b_stride < least || b_stride % 16)
         return fail(IVFPQ_EINVAL, "%s: code strides %lld, %lld: multiples of 16 of at least %lld are needed", what, (long long)a_stride, (long long)b_stride, (long long)least);
+    if ((m > 1 && a_stride > kMostStride) || (n > 1 && b_stride > kMostStride))
+        return fail(IVFPQ_EUNSUPPORTED, "%s: code strides %lld, %lld (limit 2^24)", what, (long long)a_stride, (long long)b_stride);
     if (((uintptr_t)d_a | (uintptr_t)d_b) % 16) return fail(IVFPQ_EINVAL, "%s: codes are not aligned to 16 bytes", what);
     if ((uintptr_t)d_out % value_bytes(out_dtype)) return fail(IVFPQ_EINVAL, "%s: the output is not aligned to its type", what);
     if (m > 1 && out_stride < n) return fail(IVFPQ_EINVAL, "%s: output stride %lld below n=%lld", what, (long long)out_stride, (long long)n);

@@ -96,7 +96,8 @@ def check_grad(got, want, tol):
 @pytest.mark.parametrize("n,vocab,k,temperature,pad,offset,repeats", [
     (1, 1, 1, 1.0, 0, 0, False), (3, 7, 5, 2.0, 2, 1, False), (5, 64, 64, 1.0, 0, 0, False), (4, 4097, 100, 0.5, 7, 3, False), (1, 131073, 20, 1.0, 0, 1, False),
     (8, 50001, 1024, 1.0, 0, 0, True), (1050, 515, 65, 4.0, 0, 0, True), (1100, 3001, 10, 1.0, 3, 1, False), (6, 30, 300, 1.0, 0, 0, True),
-    (3, 140000, 33, 1.0, 0, 0, False), (1030, 70001, 20, 1.0, 1, 0, False)])
+    (3, 140000, 33, 1.0, 0, 0, False), (1030, 70001, 20, 1.0, 1, 0, False),
+    (20, 50001, 100, 1.0, 0, 1, True), (17, 30000, 64, 2.0, 4, 0, False)])
 def test_loss_and_gradient(P, dtype, n, vocab, k, temperature, pad, offset, repeats):
     x = logits_of(n, vocab, dtype, seed=n + k, pad=pad, offset=offset)
     tokens, values = teacher_for(n, vocab, k, seed=vocab, repeats=repeats)

@@ -113,6 +113,43 @@ def test_layouts(P, m):
     assert torch.equal(P.ivfpq_q8_matmul(a, sa, b[::2], sb[::2], out_dtype=torch.float16).cpu(), want[:, ::2])
 
 
+@pytest.mark.parametrize("stride", [1 << 24, (1 << 24) + 16])
+def test_rows_far_apart(P, stride):
+    """Rows 2^24 bytes apart: the last of a tile's 256 begins just under 2^32 bytes from its first; farther ones are laid out anew."""
+    m, n, k = 70, 256, 144
+    room = torch.zeros(stride * (n - 1) + 144, dtype=torch.int8, device="cuda")
+    b, sb = codes_of(n, k, seed=4)
+    far = room.as_strided((n, k), (stride, 1))
+    far.copy_(b)
+    a, sa = codes_of(m, k, seed=3)
+    assert torch.equal(P.ivfpq_q8_matmul(a, sa, far, sb).cpu(), product(a, sa, b, sb, None, torch.float32))
+    many, sm = codes_of(300, k, seed=6)
+    assert torch.equal(P.ivfpq_q8_matmul(many, sm, far, sb).cpu(), product(many, sm, b, sb, None, torch.float32))
+
+
+def test_streams_and_graph(P):
+    """Captured, replays on new data give what eager calls give."""
+    x = rows_of(300, 700, torch.bfloat16, seed=1)
+    b, sb = P.ivfpq_quantize_rows(rows_of(5000, 700, torch.float32, seed=2))
+    side = torch.cuda.Stream()
+
+    def step():
+        return P.ivfpq_q8_matmul(*P.ivfpq_quantize_rows(x), b, sb, out_dtype=torch.float16)
+
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = step()
+    for seed in (10, 11, 12):
+        x.copy_(rows_of(300, 700, torch.bfloat16, seed=seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, step())
+
+
 def test_no_rows(P):
     a, sa = codes_of(4, 32, seed=1)
     none, s0 = torch.empty((0, 32), dtype=torch.int8, device="cuda"), torch.empty(0, device="cuda")

@@ -69,7 +69,8 @@ CASES = (
         (dict(dists=0), "EINVAL", "null"), (dict(table=0), "EINVAL", "null"), (dict(tokens=0), "EINVAL", "null"), (dict(logprobs=0), "EINVAL", "null")]]
     + [("ivfpq_q8_matmul", Q8, *c) for c in [
         (dict(dtype=9), "EINVAL", "dtype"), (dict(m=-1), "EINVAL", "shape"), (dict(n=-1), "EINVAL", "shape"), (dict(k=0), "EINVAL", "k=0"),
-        (dict(k=65537), "EINVAL", "k=65537"), (dict(a_stride=48), "EINVAL", "strides"), (dict(b_stride=72), "EINVAL", "strides"), (dict(a=A + 8), "EINVAL", "16 bytes"),
+        (dict(k=65537), "EINVAL", "k=65537"), (dict(a_stride=48), "EINVAL", "strides"), (dict(b_stride=72), "EINVAL", "strides"), (dict(a_stride=(1 << 24) + 16), "EUNSUPPORTED", "strides"),
+        (dict(b_stride=1 << 25), "EUNSUPPORTED", "strides"), (dict(a=A + 8), "EINVAL", "16 bytes"),
         (dict(b=A + 1), "EINVAL", "16 bytes"), (dict(out=A + 2), "EINVAL", "aligned"), (dict(out_stride=4), "EINVAL", "output stride"), (dict(a=0), "EINVAL", "null"),
         (dict(sa=0), "EINVAL", "null"), (dict(b=0), "EINVAL", "null"), (dict(sb=0), "EINVAL", "null"), (dict(out=0), "EINVAL", "null")]]
     + [("ivfpq_quantize_rows", QUANT, *c) for c in [
