@@ -22,7 +22,9 @@ namespace {
 
 constexpr int kRowThreads = 256, kRowWaves = kRowThreads / 64;
 constexpr int kMostSplits = 64;                            // workgroups that share a row
-constexpr int kMostSplitsTop = 16;                         // ... and where each leaves a list of its best keys: fewer lists are joined faster
+// ... and where each leaves a list of its best keys, which have to be joined (131,072 bf16, 20 alternatives and 64 neighbours: one row in 8, 16,
+// 32 parts 64, 36, 34 us, eight rows 64, 37, 41)
+constexpr int kMostSplitsTop = 16;
 constexpr int kMostTop = IVFPQ_MAX_MIXED;                  // keys a selection keeps
 constexpr int kCandidates = 2048 - kMostTop;               // ... and takes in before it sorts
 constexpr float kLeastPower = -150.f;                      // 2^t is 0 in fp32 below this: t is cut there before t 2^t
@@ -1120,7 +1122,7 @@ int token_logprobs(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab
     });
 }
 
-int distill_forward(const char* what, const RowsIn& in, int32_t dtype, int64_t n, const Listed& teacher, float* d_loss, float* d_norms,
+int distill_forward(const RowsIn& in, int32_t dtype, int64_t n, const Listed& teacher, float* d_loss, float* d_norms,
                     void* d_workspace, hipStream_t stream) {
     const DistillOut out{teacher, d_loss, d_norms};
     return with_value_type(dtype, [&](auto v) {
@@ -1231,7 +1233,7 @@ int ivfpq_distill_topk(const void* d_logits, int32_t dtype, int64_t n, int32_t v
         if (!d_loss || !d_norms) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
         if (int s = check_workspace(what, d_workspace, workspace_bytes, distill_scratch(n, vocab))) return s;
         void* split = (char*)d_workspace + align_up((size_t)n * 2 * sizeof(float));
-        return distill_forward(what, rows_in(d_logits, row_stride, vocab, temperature), dtype, n, Listed{d_teacher_tokens, d_teacher_logits, k},
+        return distill_forward(rows_in(d_logits, row_stride, vocab, temperature), dtype, n, Listed{d_teacher_tokens, d_teacher_logits, k},
                                d_loss, d_norms, split, (hipStream_t)hip_stream);
     });
 }
@@ -1270,7 +1272,7 @@ int ivfpq_distill_topk_step(const void* d_logits, int32_t dtype, int64_t n, int3
         const hipStream_t stream = (hipStream_t)hip_stream;
         if (step_in_registers(n, vocab, dtype))
             return distill_step(in, dtype, n, teacher, d_row_grads, d_loss, d_grad, grad_stride, stream);
-        if (int s = distill_forward(what, in, dtype, n, teacher, d_loss, norms, split, stream)) return s;
+        if (int s = distill_forward(in, dtype, n, teacher, d_loss, norms, split, stream)) return s;
         return distill_gradient(in, dtype, n, teacher, d_row_grads, norms, d_grad, grad_stride, stream);
     });
 }
