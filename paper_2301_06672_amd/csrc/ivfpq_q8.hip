@@ -136,7 +136,6 @@ __global__ __launch_bounds__(256) void skinny_kernel(Product p) {
     intx4 acc[MT][NT] = {};
     const int lines = (p.k + 127) / 128, whole = p.k / 128;
     int line = wave;
-#pragma unroll 2
     for (; line < whole; line += 4) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
