@@ -291,9 +291,10 @@ __device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long 
         }
         if constexpr (TOP)
             for (int i = tid; i < out.top; i += kRowThreads) {
-                const bool used = i < n_kept;
+                const float logp = i < n_kept ? model_logp(key_value(sel->kept[i])) : -INFINITY;
+                const bool used = logp != -INFINITY;           // a logit may be so far below the largest that this is no number of fp32
                 out.top_tokens[row * out.top + i] = used ? key_token(sel->kept[i]) : -1;
-                out.top_logprobs[row * out.top + i] = used ? model_logp(key_value(sel->kept[i])) : -INFINITY;
+                out.top_logprobs[row * out.top + i] = logp;
             }
         return;
     }

@@ -1,0 +1,68 @@
+"""Which tokens are listed as alternatives: none whose log-probability is -inf, with neighbours and without.
+
+Tolerance.  e = 2^-24: a log-probability is off by at most e (vocab / 256 + 72 + 8 |log p|), as everywhere for these rows."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+E = 2.0 ** -24
+LOWEST = {torch.float32: torch.finfo(torch.float32).min, torch.float16: -65504.0, torch.bfloat16: torch.finfo(torch.bfloat16).min}
+
+
+@pytest.fixture(scope="module")
+def P():
+    import paper_2301_06672_amd as pkg
+    pkg.lib()
+    return pkg
+
+
+def masked_rows(n, vocab, dtype, seed, fill):
+    """Rows of which 0 to 6 tokens are left by a mask of value `fill`, the last token sometimes one of them; the kept ones as truth values."""
+    gen = torch.Generator().manual_seed(seed)
+    x = (torch.randn(n, vocab, generator=gen) * 3.0).to(dtype)
+    keep = torch.zeros(n, vocab, dtype=torch.bool)
+    for r in range(n):
+        keep[r, torch.randperm(vocab, generator=gen)[: r % 7]] = True
+        if r % 3 == 1:
+            keep[r, vocab - 1] = True
+    return torch.where(keep, x, torch.tensor(fill, dtype=dtype)).cuda(), keep
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("temperature", [0.25, 0.7, 0.99, 1.0, 3.0])
+@pytest.mark.parametrize("n,vocab", [(8, 5003), (1600, 300)])                 # rows split between workgroups, and not
+def test_masked_tokens_that_no_number_holds(P, dtype, temperature, n, vocab):
+    """The lowest value of fp32 or bf16 divided by a temperature below 1 is under every fp32 number: such tokens are not listed."""
+    top = 20
+    x, keep = masked_rows(n, vocab, dtype, 3, LOWEST[dtype])
+    got = P.ivfpq_token_logprobs(x, top=top, temperature=temperature)
+    raw = x.cpu().double()
+    t = (raw - raw.amax(dim=1, keepdim=True)) / temperature
+    logp = t - torch.logsumexp(t, dim=1, keepdim=True)
+    listed = logp > -3.4028235677973366e38                                    # what rounds to a number in fp32
+    order = torch.where(listed, raw, -math.inf)
+    values, tokens = torch.sort(order, dim=1, descending=True, stable=True)
+    values, tokens = values[:, :top], tokens[:, :top]
+    tokens = torch.where(values > -math.inf, tokens, -1).int()
+    if temperature < 1.0 and dtype != torch.float16:
+        some = keep.any(dim=1)
+        assert ((tokens >= 0).sum(dim=1)[some] == keep.sum(dim=1)[some]).all()
+    assert torch.equal(got.top_tokens.cpu(), tokens)
+    lp = torch.where(tokens >= 0, logp.gather(1, tokens.clamp(min=0).long()), -math.inf)
+    have = got.top_logprobs.cpu().double()
+    assert torch.equal(have == -math.inf, tokens < 0)
+    there = tokens >= 0
+    assert bool(((have - lp)[there].abs() <= E * (vocab / 256 + 72 + 8 * lp[there].abs())).all())
+
+
+@pytest.mark.parametrize("n", [5, 1600])
+def test_the_same_tokens_with_neighbours_that_add_nothing(P, n):
+    """A mixture whose listed tokens are unused lists what the model alone does."""
+    x, _ = masked_rows(n, 700, torch.bfloat16, 5, LOWEST[torch.bfloat16])
+    none = torch.full((n, 12), -1, dtype=torch.int32, device="cuda"), torch.full((n, 12), -math.inf, device="cuda")
+    alone = P.ivfpq_token_logprobs(x, top=30, temperature=0.5)
+    mixed = P.ivfpq_token_logprobs(x, top=30, temperature=0.5, neighbours=none, weight=0.5)
+    assert torch.equal(alone.top_tokens, mixed.top_tokens) and torch.equal(alone.top_logprobs, mixed.top_logprobs)
