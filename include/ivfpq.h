@@ -324,7 +324,8 @@ int ivfpq_neighbour_tokens(const int64_t* d_ids, const float* d_dists, int64_t n
  *   d_logprobs [n]: of d_targets, 0 for a target outside [0, vocab); NULL if and only if d_targets is
  *   d_entropy [n] (nats), d_norms [n][2]: may be NULL
  *   d_top_tokens, d_top_logprobs [n][top]: descending, ties to the lower token; tokens whose log-probability is -inf (p = 0, or
- *   log p below every fp32 number) are not listed, and unused places hold -1 and -inf.  The order of the model's own distribution is that of the logits.  0 <= top <= IVFPQ_MAX_TOP.
+ *   log p below every fp32 number) are not listed, and unused places hold -1 and -inf (-1 and NaN in a row of NaN statistics, whose
+ *   tokens are of no meaning).  The order of the model's own distribution is that of the logits.  0 <= top <= IVFPQ_MAX_TOP.
  * n_neighbours > 0 mixes the rows' distributions with listed ones (ivfpq_neighbour_tokens): (1 - weight) p + weight q,
  * 0 < weight < 1, q given by d_neighbour_tokens and d_neighbour_logprobs [n][n_neighbours]; the used tokens of a row are
  * distinct.  Log-probabilities, entropy and alternatives are then the mixture's (norms stay the model's).  A row without

@@ -282,6 +282,7 @@ __device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long 
     // log p of a logit
     auto model_logp = [&](float v) { return none ? -INFINITY : (v - sum.m) / in.temperature - log_s; };
     const float entropy = none ? 0.f : log_s - kLn2 * (sum.u / sum.s);
+    const float unused = sum.s != sum.s ? sum.s : -INFINITY;       // in the place of an alternative: a row of NaN statistics has no other
     if (tid == 0) write_norms(out.norms, row, sum.m, log_s, none);
 
     if (out.near.k == 0) {
@@ -291,8 +292,8 @@ __device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long 
         }
         if constexpr (TOP)
             for (int i = tid; i < out.top; i += kRowThreads) {
-                const float logp = i < n_kept ? model_logp(key_value(sel->kept[i])) : -INFINITY;
-                const bool used = logp != -INFINITY;           // a logit may be so far below the largest that this is no number of fp32
+                const float logp = i < n_kept ? model_logp(key_value(sel->kept[i])) : unused;
+                const bool used = i < n_kept && logp != -INFINITY;       // a logit may be so far below the largest that this is no number of fp32
                 out.top_tokens[row * out.top + i] = used ? key_token(sel->kept[i]) : -1;
                 out.top_logprobs[row * out.top + i] = logp;
             }
@@ -366,7 +367,7 @@ __device__ inline void finish_score(const RowsIn& in, const ScoreOut& out, long 
         for (int i = tid; i < out.top; i += kRowThreads) {
             const bool used = i < best && sel->kept[i];
             out.top_tokens[row * out.top + i] = used ? key_token(sel->kept[i]) : -1;
-            out.top_logprobs[row * out.top + i] = used ? key_value(sel->kept[i]) : -INFINITY;
+            out.top_logprobs[row * out.top + i] = used ? key_value(sel->kept[i]) : unused;
         }
     }
 }

@@ -66,3 +66,24 @@ def test_the_same_tokens_with_neighbours_that_add_nothing(P, n):
     alone = P.ivfpq_token_logprobs(x, top=30, temperature=0.5)
     mixed = P.ivfpq_token_logprobs(x, top=30, temperature=0.5, neighbours=none, weight=0.5)
     assert torch.equal(alone.top_tokens, mixed.top_tokens) and torch.equal(alone.top_logprobs, mixed.top_logprobs)
+
+
+@pytest.mark.parametrize("n", [6, 1600])
+def test_rows_without_statistics_have_no_log_probabilities(P, n):
+    """A NaN or +inf among a row's logits: NaN for every alternative, with neighbours and without, and the other rows as they were."""
+    gen = torch.Generator().manual_seed(7)
+    clean = (torch.randn(n, 3000, generator=gen) * 3.0).cuda()
+    x = clean.clone()
+    x[0, 2999], x[2, 17], x[3] = math.nan, math.inf, math.nan
+    x[5, :2995] = -math.inf
+    clean[5] = x[5]
+    x[5, 2998] = math.nan
+    tokens = torch.arange(12, dtype=torch.int32, device="cuda").repeat(n, 1) * 100
+    logq = torch.log_softmax(torch.randn(n, 12, generator=gen), dim=1).cuda()
+    bad = torch.zeros(n, dtype=torch.bool, device="cuda")
+    bad[[0, 2, 3, 5]] = True
+    for near, weight in ((None, 0.0), ((tokens, logq), 0.25)):
+        got = P.ivfpq_token_logprobs(x, top=20, neighbours=near, weight=weight)
+        want = P.ivfpq_token_logprobs(clean, top=20, neighbours=near, weight=weight)
+        assert torch.isnan(got.top_logprobs[bad]).all() and torch.isnan(got.entropy[bad]).all()
+        assert torch.equal(got.top_logprobs[~bad], want.top_logprobs[~bad]) and torch.equal(got.top_tokens[~bad], want.top_tokens[~bad])
