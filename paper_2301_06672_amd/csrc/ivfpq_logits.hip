@@ -476,7 +476,9 @@ __device__ inline void largest_of_chunks(const Chunk<T> (&k)[N], float (&most)[N
 
 // Adds the chunks to a thread's sums; leaves the maximum of every chunk, and of all so far in `largest`.  The reference follows the
 // maximum only when that is over 2^kSlack of it: most tiles raise some lane's maximum by a little, and a raise costs as
-// much as an element.  The sums' parts stay within 2^kSlack of their place, so nothing is lost.
+// much as an element.  The sums' parts stay within 2^kSlack of their place, so nothing is lost.  A tile's values are added up among
+// themselves first: one after the other onto a sum near its end, small ones are rounded away (65,536 normal logits, in log S: 3.5e-7 too
+// little on average against 0.6e-7).
 constexpr float kSlack = 4.f;
 template <class T, bool ENTROPY, int N>
 __device__ inline void add_tile(Chunk<T> (&k)[N], float scale, RowSum& sum, float& largest, float (&most)[N]) {
@@ -492,14 +494,20 @@ __device__ inline void add_tile(Chunk<T> (&k)[N], float scale, RowSum& sum, floa
     }
     if ((largest - sum.m) * scale > kSlack) sum.raise(largest, scale);
     const float ref = sum.m == -INFINITY ? 0.f : sum.m;     // nothing but -inf so far: t = -inf, not a NaN
+    float s[N], u[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < N; ++i) {
+        float e[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            const float t = (x[i][j] - ref) * scale, e = exp2_fast(t);
-            sum.s += e;
-            if constexpr (ENTROPY) sum.u = __builtin_fmaf(fmaxf(t, kLeastPower), e, sum.u);
+            const float t = (x[i][j] - ref) * scale;
+            e[j] = exp2_fast(t);
+            if constexpr (ENTROPY) u[i] = j ? __builtin_fmaf(fmaxf(t, kLeastPower), e[j], u[i]) : fmaxf(t, kLeastPower) * e[j];
         }
+        s[i] = tree_sum<VEC>(e);
+    }
+    sum.s += tree_sum<N>(s);
+    if constexpr (ENTROPY) sum.u += tree_sum<N>(u);
 }
 
 // The largest key of a thread's chunks, 0 if they hold nothing above -inf.
@@ -943,7 +951,8 @@ __global__ __launch_bounds__(THREADS) void distill_step_kernel(RowsIn in, Distil
         k.forget_widened();
         k.widen(x);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) s += exp2_fast((x[j] - ref) * in.scale);
+        for (int j = 0; j < VEC; ++j) x[j] = exp2_fast((x[j] - ref) * in.scale);
+        s += tree_sum<VEC>(x);
     };
     if (front || back) add(edge[0]);
 #pragma unroll

@@ -113,6 +113,13 @@ __device__ inline float max3(float a, float b, float c) {
     return d;
 }
 
+// The sum of N values, halves added up apart
+template <int N>
+__device__ inline float tree_sum(const float* x) {
+    if constexpr (N == 1) return x[0];
+    else return tree_sum<N / 2>(x) + tree_sum<N - N / 2>(x + N / 2);
+}
+
 // The sum over a workgroup of THREADS, in every thread; the order of additions is fixed.  `scratch`: THREADS / 64 words that no
 // wave still reads; they are free again after the next barrier.
 template <int THREADS, class V>
