@@ -216,9 +216,16 @@ def _plain(what: str, t: torch.Tensor, dtype, *shape):
     return t.contiguous()
 
 
+def _fits_int32(what: str, size: int):
+    """Row lengths are int32 in the C ABI, and ctypes cuts what is over that without a word."""
+    if size > 2 ** 31 - 1:
+        _refuse(f"{what}: rows of {size} values (limit 2^31 - 1)")
+
+
 def _value_rows(what: str, x: torch.Tensor) -> torch.Tensor:
     if x.dim() != 2 or x.dtype not in VALUES_DTYPES:
         _refuse(f"{what}: expected a matrix of float32, float16 or bfloat16, got {x.dtype} {tuple(x.shape)}")
+    _fits_int32(what, x.shape[1])
     return x if _rows_apart(x) else x.contiguous()
 
 
@@ -241,6 +248,7 @@ def _listed(what: str, tokens: torch.Tensor, values: torch.Tensor, n: int):
     if tokens.dim() != 2:
         _refuse(f"{what}: listed tokens are a matrix")
     k = tokens.shape[1]
+    _fits_int32(what, k)
     return _plain(what, tokens, torch.int32, n, k), _plain(what, values, torch.float32, n, k)
 
 
@@ -268,6 +276,7 @@ def _code_rows(what: str, codes: torch.Tensor):
     if codes.dim() != 2 or codes.dtype != torch.int8:
         _refuse(f"{what}: codes are a matrix of int8, got {codes.dtype} {tuple(codes.shape)}")
     n, k = codes.shape
+    _fits_int32(what, k)
     width = -(-k // 16) * 16
     stride = codes.stride(0) if n > 1 else width
     fits = (k <= 1 or codes.stride(1) == 1) and stride % 16 == 0 and width <= stride <= 1 << 24 and codes.data_ptr() % 16 == 0 and (
@@ -309,6 +318,7 @@ def ivfpq_neighbour_tokens(ids: torch.Tensor, dists: torch.Tensor, id_tokens: to
     if ids.dim() != 2:
         _refuse(f"{what}: ids are a matrix")
     nq, k = ids.shape
+    _fits_int32(what, k)
     ids, dists = _plain(what, ids, torch.int64, nq, k), _plain(what, dists, torch.float32, nq, k)
     table = _plain(what, id_tokens, torch.int32, id_tokens.numel())
     tokens = torch.empty((nq, k), dtype=torch.int32, device="cuda")
@@ -325,6 +335,8 @@ def ivfpq_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] =
     _on_device(what, logits, targets, *(neighbours or ()))
     x = _value_rows(what, logits)
     n, vocab = x.shape
+    if not 0 <= top <= MAX_TOP:
+        _refuse(f"{what}: top={top} outside [0, {MAX_TOP}]")
     targets = None if targets is None else _plain(what, targets, torch.int32, n)
     near_tokens, near_logprobs = (None, None) if neighbours is None else _listed(what, *neighbours, n)
     k = 0 if near_tokens is None else near_tokens.shape[1]
