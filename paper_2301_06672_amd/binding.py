@@ -410,8 +410,8 @@ def ivfpq_distill_topk_step(logits: torch.Tensor, teacher_tokens: torch.Tensor, 
     n, vocab = x.shape
     tokens, values = _listed(what, teacher_tokens, teacher_logits, n)
     row_grads = None if row_grads is None else _plain(what, row_grads, torch.float32, n)
-    loss = torch.empty(n, dtype=torch.float32, device="cuda")
     grad = _grad_like(what, x, out)
+    loss = torch.empty(n, dtype=torch.float32, device="cuda")
     need = lib().ivfpq_distill_topk_workspace_bytes(n, vocab)
     ws = _scratch(need)
     _check(lib().ivfpq_distill_topk_step(*_logits(x), _dp(tokens), _dp(values), tokens.shape[1], temperature, _dp(row_grads), _dp(loss),
