@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "ivfpq_hip_util.hpp"
+#include "ivfpq_language_rules.hpp"
 #include "ivfpq_values.hpp"
 
 using namespace ivfpq;
@@ -370,22 +371,14 @@ int launch_tiles(const Product& p, hipStream_t stream) {
 constexpr int64_t kPiece = 1 << 22;        // rows of one launch: fewer than 2^32 threads
 constexpr int64_t kMostStride = 1 << 24;   // 255 of them and a piece's place in its line are a 32-bit offset from a tile's first row
 
-// Few rows of a, or few outputs: the tiles of 128 x 128 would leave most of the GPU idle (measured with k = 4096, a of 32 rows: n = 4,000
-// 8.6 against 20 us, 16,000 19 against 23, 32,768 34 against 25; of 64 rows: n = 8,000 17 against 23, 32,768 52 against 27).
-// Two blocks of b a wave where enough waves are left (32 rows: n = 32,768 34 against 46 us, 4,000 11 against 8.6).
 template <class T>
 int launch_product(const Product& p, hipStream_t stream) {
-    const int64_t strips = (p.m <= 32 ? 2 : (p.m + 63) / 64 * (int64_t)4) * p.n;       // blocks of 16 rows that the waves would multiply, times n
-    if (p.m <= 16 || strips <= 40000) {
-        const bool wide = p.n >= 8192;
-        if (p.m <= 16) return wide ? launch_skinny<T, 1, 2>(p, stream) : launch_skinny<T, 1, 1>(p, stream);
-        if (p.m <= 32) return wide ? launch_skinny<T, 2, 2>(p, stream) : launch_skinny<T, 2, 1>(p, stream);
-        return wide ? launch_skinny<T, 4, 2>(p, stream) : launch_skinny<T, 4, 1>(p, stream);
-    }
-    // tiles of 256 x 256 where the GPU has one for every CU (1,000 x 30,000, k = 900: 63 us against 83; 512 x 32,768, k = 4,096: 75 against 86),
-    // but for sums of few slices, whose time is the stores: more, smaller workgroups overlap them (777 x 100,003, k = 96: 75 against 87)
-    if (p.k > 256 && (int64_t)((p.m + 255) / 256) * ((p.n + 255) / 256) >= 256) return launch_tiles<T, 256, 256, 2, 4>(p, stream);
-    return launch_tiles<T, 128, 128, 2, 2>(p, stream);
+    const ProductKernel kernel = product_kernel(p.m, p.n, p.k);
+    if (kernel.tiles) return kernel.rows == 256 ? launch_tiles<T, 256, 256, 2, 4>(p, stream) : launch_tiles<T, 128, 128, 2, 2>(p, stream);
+    const bool wide = kernel.columns == 32;
+    if (kernel.rows == 16) return wide ? launch_skinny<T, 1, 2>(p, stream) : launch_skinny<T, 1, 1>(p, stream);
+    if (kernel.rows == 32) return wide ? launch_skinny<T, 2, 2>(p, stream) : launch_skinny<T, 2, 1>(p, stream);
+    return wide ? launch_skinny<T, 4, 2>(p, stream) : launch_skinny<T, 4, 1>(p, stream);
 }
 
 int q8_matmul(const int8_t* d_a, int64_t a_stride, const float* d_a_scales, int64_t m, const int8_t* d_b, int64_t b_stride,

@@ -1,0 +1,63 @@
+"""CPU checks of the rules that choose the kernels of the language-model calls: the library's own header, compiled on the spot."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+import util_products
+
+SHIM = """
+#include "ivfpq_language_rules.hpp"
+extern "C" int product(long long m, long long n, int k, int* rows, int* columns) {
+    const ivfpq::ProductKernel c = ivfpq::product_kernel(m, n, k);
+    *rows = c.rows;
+    *columns = c.columns;
+    return c.tiles;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def rules(tmp_path_factory):
+    where = tmp_path_factory.mktemp("rules")
+    (where / "shim.cpp").write_text(SHIM)
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2301_06672_amd", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-I", csrc, str(where / "shim.cpp"), "-o", str(where / "shim.so")], check=True)
+    lib = ctypes.CDLL(str(where / "shim.so"))
+    lib.product.argtypes = [ctypes.c_longlong, ctypes.c_longlong, ctypes.c_int] + [ctypes.POINTER(ctypes.c_int)] * 2
+    return lib
+
+
+def product(rules, m, n, k):
+    rows, columns = ctypes.c_int(), ctypes.c_int()
+    tiles = rules.product(m, n, k, rows, columns)
+    return bool(tiles), rows.value, columns.value
+
+
+def test_products_that_were_measured(rules):
+    # the faster side of every figure at the rule
+    for m, n, k, tiles, rows in [(32, 4000, 4096, False, 32), (32, 16000, 4096, False, 32), (32, 32768, 4096, True, 128), (64, 8000, 4096, False, 64),
+                                 (64, 32768, 4096, True, 128), (1000, 30000, 900, True, 256), (512, 32768, 4096, True, 256), (777, 100003, 96, True, 128),
+                                 (1, 32768, 4096, False, 16), (2048, 32768, 4096, True, 256)]:
+        assert product(rules, m, n, k)[:2] == (tiles, rows), (m, n, k)
+    assert product(rules, 32, 4000, 4096)[2] == 16 and product(rules, 16, 32768, 4096)[2] == 32
+
+
+def test_sizes_of_the_tests_of_tiles_take_tiles(rules):
+    for m, n, k, tile, aligned in util_products.TILES:
+        assert product(rules, m, n, k) == (True, tile, tile), (m, n, k)
+        assert aligned == (4 * n % 64 == 0, 2 * n % 64 == 0)
+    for m, n, k, tile in util_products.LAYOUTS:
+        assert product(rules, m, n, k) == (True, tile, tile), (m, n, k)
+    for far, m, n, k, tile in util_products.FAR:
+        assert product(rules, m, n, k) == (True, tile, tile), (m, n, k)
+        assert (m if far == "a" else n) >= tile
+
+
+@pytest.mark.parametrize("m", [1, 16, 17, 32, 33, 64, 65, 4096, 1 << 22])
+@pytest.mark.parametrize("n", [1, 16, 8191, 8192, 40000, 1 << 22])
+def test_strips_have_a_launch(rules, m, n):
+    """A grid's second dimension ends at 65,535."""
+    tiles, rows, columns = product(rules, m, n, 64)
+    assert tiles or (-(-m // rows) <= 65535 and rows in (16, 32, 64) and columns in (16, 32))
