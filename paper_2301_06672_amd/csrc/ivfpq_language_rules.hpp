@@ -23,4 +23,22 @@ inline ProductKernel product_kernel(int64_t m, int64_t n, int k) {
     return {true, 128, 128};
 }
 
+// Whether a distillation step holds every row in the registers of one workgroup (kHeldChunks pieces of 16 bytes a thread, up to 1,024 threads): one
+// launch and one read of the logits instead of three and two, but a row in 1 of 256 compute units, where the split kernels take as many as there
+// are.  One row's time grows with its values, whatever their type; 16-bit rows have up to 131,072 of them, fp32 rows 65,536.  us, registers / split,
+// called one after the other from Python (where three launches take 19 us of the host) and replayed from a graph:
+//   bf16 values            called    1 row        16           48           96           160          replayed   1            16           48           96           160
+//   50,000                 13.8 / 19.1  14.0 / 19.3  15.5 / 19.0  18.9 / 20.1  20.7 / 25.5            12.0 / 12.0  13.4 / 14.3  15.6 / 17.7  19.5 / 20.7  21.1 / 25.8
+//   65,536                 13.9 / 18.8  16.0 / 19.1  17.2 / 19.1  22.0 / 22.7  23.6 / 27.1            13.8 / 11.7  16.4 / 15.1  18.0 / 17.7  22.8 / 23.2  23.6 / 27.4
+//   80,000                 15.8 / 18.9  18.1 / 19.1  19.6 / 19.1  23.1 / 25.0  24.8 / 29.3            15.6 / 11.9  18.6 / 15.5  20.1 / 18.3  23.5 / 25.3  25.0 / 29.7
+//   100,000                18.3 / 18.9  21.1 / 19.2  24.6 / 19.6  26.9 / 25.6  28.2 / 33.3            17.7 / 11.9  21.2 / 16.4  25.3 / 20.0  27.2 / 26.0  28.8 / 33.9
+//   131,072                24.0 / 18.8  24.9 / 19.0  30.6 / 22.5  32.3 / 28.8  34.3 / 39.1            23.5 / 12.4  25.3 / 16.3  30.7 / 23.1  32.5 / 29.0  34.9 / 39.7
+//   fp32: 65,536           13.6 / 18.9  13.8 / 19.2  17.5 / 21.5  20.1 / 27.6  24.9 / 38.0            12.6 / 12.1  13.3 / 15.6  17.6 / 21.9  20.1 / 27.9  25.2 / 38.6
+// 4,096 rows of 65,536 bf16 values: 266 / 372.
+constexpr int kHeldChunks = 16;
+inline bool step_in_registers(int64_t n, int64_t vocab, int value_bytes) {
+    if (vocab * value_bytes > (int64_t)16 * kHeldChunks * 1024) return false;
+    return vocab <= 80000 || n >= 112;
+}
+
 }  // namespace ivfpq

@@ -14,6 +14,7 @@
 
 #include "ivfpq_float_key.hpp"
 #include "ivfpq_hip_util.hpp"
+#include "ivfpq_language_rules.hpp"
 #include "ivfpq_values.hpp"
 
 using namespace ivfpq;
@@ -910,8 +911,8 @@ __global__ __launch_bounds__(kRowThreads) void row_gradient_kernel(RowsIn in, Gr
 }
 
 // Loss and gradient in one pass, for rows that fit the registers of a workgroup (HELD 16-byte chunks a thread): every
-// logit is read once and every element of the gradient written once.  4,096 x 65,536 bf16: 260 us, 4.1 TB/s (a copy: 4.65); two
-// workgroups a CU, so that one row's loads run beside the other's exponentials and stores.
+// logit is read once and every element of the gradient written once.  4,096 x 65,536 bf16 (512 threads): 260 us, 4.1 TB/s (a copy: 4.65); two
+// workgroups a CU, so that one row's loads run beside the other's exponentials and stores.  Of 1,024 threads a CU holds one.
 template <class T, int THREADS, int HELD>
 __global__ __launch_bounds__(THREADS) void distill_step_kernel(RowsIn in, DistillGrad how, float* __restrict__ loss, void* grads, long long grad_stride) {
     constexpr int VEC = Chunk<T>::VEC;
@@ -1151,14 +1152,6 @@ int distill_gradient(const RowsIn& in, int32_t dtype, int64_t n, const Listed& t
     return with_value_type(dtype, [&](auto v) { return launch_gradient<decltype(v), false>(n, in, g, how, stream); });
 }
 
-// Rows in registers where they fit: one launch and one read of the logits instead of three and two (4,096 x 65,536 bf16: 266 against
-// 372 us).  A few long rows are better split between many workgroups.
-constexpr int kHeldChunks = 16;
-bool step_in_registers(int64_t n, int32_t vocab, int32_t dtype) {
-    const int64_t bytes = (int64_t)vocab * value_bytes(dtype);
-    return bytes <= (int64_t)16 * kHeldChunks * 1024 && (n >= 16 || bytes <= 65536);
-}
-
 template <class T, int THREADS, int HELD>
 int launch_step(int64_t n, const RowsIn& in, const DistillGrad& how, float* d_loss, void* d_grad, int64_t grad_stride, hipStream_t stream) {
     hipLaunchKernelGGL((distill_step_kernel<T, THREADS, HELD>), dim3((unsigned)n), dim3(THREADS), 0, stream, in, how, d_loss, d_grad, (long long)grad_stride);
@@ -1281,7 +1274,7 @@ int ivfpq_distill_topk_step(const void* d_logits, int32_t dtype, int64_t n, int3
         const RowsIn in = rows_in(d_logits, row_stride, vocab, temperature);
         const Listed teacher{d_teacher_tokens, d_teacher_logits, k};
         const hipStream_t stream = (hipStream_t)hip_stream;
-        if (step_in_registers(n, vocab, dtype))
+        if (step_in_registers(n, vocab, value_bytes(dtype)))
             return distill_step(in, dtype, n, teacher, d_row_grads, d_loss, d_grad, grad_stride, stream);
         if (int s = distill_forward(in, dtype, n, teacher, d_loss, norms, split, stream)) return s;
         return distill_gradient(in, dtype, n, teacher, d_row_grads, norms, d_grad, grad_stride, stream);

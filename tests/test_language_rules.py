@@ -15,6 +15,7 @@ extern "C" int product(long long m, long long n, int k, int* rows, int* columns)
     *columns = c.columns;
     return c.tiles;
 }
+extern "C" int in_registers(long long n, long long vocab, int value_bytes) { return ivfpq::step_in_registers(n, vocab, value_bytes); }
 """
 
 
@@ -26,6 +27,7 @@ def rules(tmp_path_factory):
     subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-I", csrc, str(where / "shim.cpp"), "-o", str(where / "shim.so")], check=True)
     lib = ctypes.CDLL(str(where / "shim.so"))
     lib.product.argtypes = [ctypes.c_longlong, ctypes.c_longlong, ctypes.c_int] + [ctypes.POINTER(ctypes.c_int)] * 2
+    lib.in_registers.argtypes = [ctypes.c_longlong, ctypes.c_longlong, ctypes.c_int]
     return lib
 
 
@@ -61,3 +63,20 @@ def test_strips_have_a_launch(rules, m, n):
     """A grid's second dimension ends at 65,535."""
     tiles, rows, columns = product(rules, m, n, 64)
     assert tiles or (-(-m // rows) <= 65535 and rows in (16, 32, 64) and columns in (16, 32))
+
+
+# distillation steps called one after the other, us: rows, values, bytes of one, in registers, split
+STEPS = [(1, 32000, 2, 11.2, 11.7), (1, 50000, 2, 13.8, 19.1), (64, 50000, 2, 15.8, 19.0), (8, 65536, 2, 14.5, 19.2), (32, 65536, 2, 17.1, 19.1), (160, 65536, 2, 23.6, 27.1),
+         (1, 80000, 2, 15.8, 18.9), (24, 80000, 2, 18.4, 19.1), (96, 80000, 2, 23.1, 25.0), (16, 100000, 2, 21.1, 19.2), (48, 100000, 2, 24.6, 19.6),
+         (96, 100000, 2, 26.9, 25.6), (128, 100000, 2, 27.6, 29.2), (1, 131072, 2, 24.0, 18.8), (16, 131072, 2, 24.9, 19.0), (32, 131072, 2, 26.5, 19.1),
+         (64, 131072, 2, 30.4, 25.3), (96, 131072, 2, 32.3, 28.8), (128, 131072, 2, 32.4, 33.8), (160, 131072, 2, 34.3, 39.1), (1, 50000, 4, 13.6, 18.8),
+         (1, 65536, 4, 13.6, 18.9), (16, 65536, 4, 13.8, 19.2), (160, 65536, 4, 24.9, 38.0), (4096, 65536, 2, 266.0, 372.0)]
+
+
+@pytest.mark.parametrize("n,vocab,size,held,split", STEPS)
+def test_steps_that_were_measured(rules, n, vocab, size, held, split):
+    assert bool(rules.in_registers(n, vocab, size)) == (held < split)
+
+
+def test_rows_that_no_registers_hold(rules):
+    assert not rules.in_registers(4096, 131073, 2) and not rules.in_registers(4096, 65537, 4) and rules.in_registers(4096, 131072, 2)
