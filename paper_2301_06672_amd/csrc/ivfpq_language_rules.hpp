@@ -34,10 +34,12 @@ inline ProductKernel product_kernel(int64_t m, int64_t n, int k) {
 //   100,000                18.3 / 18.9  21.1 / 19.2  24.6 / 19.6  26.9 / 25.6  28.2 / 33.3            17.7 / 11.9  21.2 / 16.4  25.3 / 20.0  27.2 / 26.0  28.8 / 33.9
 //   131,072                24.0 / 18.8  24.9 / 19.0  30.6 / 22.5  32.3 / 28.8  34.3 / 39.1            23.5 / 12.4  25.3 / 16.3  30.7 / 23.1  32.5 / 29.0  34.9 / 39.7
 //   fp32: 65,536           13.6 / 18.9  13.8 / 19.2  17.5 / 21.5  20.1 / 27.6  24.9 / 38.0            12.6 / 12.1  13.3 / 15.6  17.6 / 21.9  20.1 / 27.9  25.2 / 38.6
-// 4,096 rows of 65,536 bf16 values: 266 / 372.
+// 4,096 rows of 65,536 bf16 values: 266 / 372.  Where the two ways of calling disagree, which is for few 16-bit rows of over 50,000 values, rows stay
+// split below 16 of them and held from there on.
 constexpr int kHeldChunks = 16;
 inline bool step_in_registers(int64_t n, int64_t vocab, int value_bytes) {
     if (vocab * value_bytes > (int64_t)16 * kHeldChunks * 1024) return false;
+    if (n < 16) return value_bytes == 4 || vocab <= 50000;
     return vocab <= 80000 || n >= 112;
 }
 
