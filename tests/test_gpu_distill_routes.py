@@ -17,7 +17,8 @@ def P():
 
 @pytest.mark.parametrize("dtype,n,vocab", [
     (torch.bfloat16, 5, 80000), (torch.bfloat16, 5, 80001), (torch.bfloat16, 111, 80001), (torch.bfloat16, 112, 80001), (torch.float16, 16, 131072),
-    (torch.float16, 112, 131072), (torch.float16, 112, 131073), (torch.float32, 1, 65536), (torch.float32, 3, 65536), (torch.float32, 3, 65537)])
+    (torch.float16, 112, 131072), (torch.float16, 112, 131073), (torch.bfloat16, 15, 50000), (torch.bfloat16, 15, 50001), (torch.float16, 16, 50001),
+    (torch.float32, 1, 65536), (torch.float32, 3, 65536), (torch.float32, 3, 65537)])
 @pytest.mark.parametrize("offset", [0, 1])
 def test_both_sides(P, dtype, n, vocab, offset):
     gen = torch.Generator(device="cuda").manual_seed(n + vocab)
