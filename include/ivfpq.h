@@ -342,8 +342,8 @@ int ivfpq_token_logprobs(const void* d_logits, int32_t dtype, int64_t n, int32_t
 /* Gradient with respect to the logits of sum_i g_i logprob_i + h_i entropy_i (the model's own distribution, no
  * mixture), g = d_grad_logprobs [n], h = d_grad_entropy [n]; either may be NULL (zeros), not both:
  *   grad[v] = (g (v == target) - g p_v - h p_v (log p_v + entropy)) / T,  g of a target outside [0, vocab) counted as 0.
- * d_norms, d_entropy: of the forward call on the same logits, targets and temperature (d_entropy may be NULL without
- * d_grad_entropy, d_targets without d_grad_logprobs).  d_grad [n][vocab] of the logits' dtype. */
+ * d_norms, d_entropy: of a forward call without neighbours (a mixture's entropy is another) on the same logits and temperature.
+ * d_entropy may be NULL without d_grad_entropy, d_targets without d_grad_logprobs.  d_grad [n][vocab] of the logits' dtype. */
 int ivfpq_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t n, int32_t vocab, int64_t row_stride,
                                   const int32_t* d_targets, float temperature, const float* d_norms, const float* d_entropy,
                                   const float* d_grad_logprobs, const float* d_grad_entropy, void* d_grad,

@@ -354,7 +354,8 @@ def ivfpq_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] =
 def ivfpq_token_logprobs_backward(logits: torch.Tensor, targets: Optional[torch.Tensor], norms: torch.Tensor, entropy: Optional[torch.Tensor],
                                   grad_logprobs: Optional[torch.Tensor], grad_entropy: Optional[torch.Tensor] = None,
                                   temperature: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """-> the gradient with respect to the logits (written to `out`, which may be the logits themselves)."""
+    """-> the gradient with respect to the logits (written to `out`, which may be the logits themselves); norms and entropy of a call
+    without neighbours."""
     what = "ivfpq_token_logprobs_backward"
     _on_device(what, logits, targets, norms, entropy, grad_logprobs, grad_entropy)
     x = _value_rows(what, logits)

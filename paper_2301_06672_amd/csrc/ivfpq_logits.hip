@@ -3,9 +3,10 @@
 //
 // Everything a row needs is a sum over exp2(t), t = (x - M) log2(e) / T with M the row's largest logit:
 //   S = sum 2^t,  U = sum t 2^t,   log p_v = ln2 (t_v - log2 S),   entropy = ln2 (log2 S - U / S).
-// Both terms of the entropy are non-negative (t <= 0), so nothing cancels.  Partial results (m, s, u) about an own maximum m
-// combine by shifting: s 2^d, (u + d s) 2^d, d = (m - M) log2(e) / T.  One pass over the logits is enough, and a row can be
-// split between workgroups.  x - M is formed before the scale: a fused x scale - M scale would save one of eleven
+// t <= 0, so both terms of the entropy are non-negative.  Partial results (m, s, u) about a reference m combine by
+// shifting: s 2^d, (u + d s) 2^d, d = (m - M) log2(e) / T.  A thread's reference may be up to 2^kSlack below its largest logit until its last
+// shift; t is at most kSlack there, and the terms that cancel in u + d s are at most kSlack s each.  One pass over the logits is
+// enough, and a row can be split between workgroups.  x - M is formed before the scale: a fused x scale - M scale would save one of eleven
 // operations an element, but leaves fp32 where a row has nothing but masks of the type's lowest value.
 #include <hip/hip_runtime.h>
 
@@ -624,10 +625,11 @@ __device__ inline int select_step_by_step(const RowChunks<T>& row, int begin, in
 // those is collected from the next tiles without a barrier, merged after 4, 16, ... tiles (a bound from N tiles lets about as
 // many of the next N pass as are wanted).
 //
-// Measured on bf16: 4,096 x 65,536 without entropy 105 us (5.1 TB/s), with entropy and 20 alternatives 117 us (4.6 TB/s); 2,048 rows with
-// entropy 55 us (4.9 TB/s).  Reading bounds the first; the others are near what the vector ALU takes, about ten instructions
-// and an exponential (of two) a logit.  Tiles of two chunks a thread: of four, alternatives take 1.5 times as long (registers: five workgroups a
-// CU for six, and more to look through).
+// Measured on bf16, calls in a row, inputs of over 1 GB in turn: 4,096 x 65,536 without entropy 99 us (5.4 TB/s), with entropy 101, with
+// 20 alternatives too 135 (4.0 TB/s: normal logits in any order; 115 where the likely tokens are the low ones, whose bounds let fewer pass);
+// 2,048 rows with entropy 55 us (4.9 TB/s), 80 right after a kernel that wrote as much.  Reading bounds the first; the others are near what
+// the vector ALU takes, about ten instructions and an exponential (of two) a logit.  Tiles of two chunks a thread: of four, alternatives
+// take 1.5 times as long (registers: five workgroups a CU for six, and more to look through).
 template <class T, RowMode MODE, class Out>
 __global__ __launch_bounds__(kRowThreads, 6) void row_statistics_kernel(RowsIn in, RowSplit split, Out out) {
     constexpr int VEC = Chunk<T>::VEC;
@@ -719,7 +721,7 @@ __global__ __launch_bounds__(kRowThreads, 6) void row_statistics_kernel(RowsIn i
 }
 
 // One workgroup a row: joins what the row's workgroups left.  A chain of latencies: one row of 131,072 with 20 alternatives mixed with
-// 64 neighbours 15 us beside the 18 us of its statistics.
+// 64 neighbours 16 us beside the 18 us of its statistics.
 template <class T, RowMode MODE, class Out>
 __global__ __launch_bounds__(kRowThreads) void row_join_kernel(RowsIn in, RowSplit split, Out out) {
     __shared__ RowLds<MODE> lds;
@@ -837,7 +839,7 @@ __device__ inline void write_listed(int k, int token0, int token1, const GradSha
 // grad_v = p_v (a + b t_v), t_v = log2 p_v, plus a term at a few listed tokens; a row without a distribution has zeros.
 // One workgroup: the chunks [split * chunks, ...) of a row.  The listed tokens' logits are read before anything is
 // written (the gradient may lie over the logits) and their elements written again after a barrier.  Bound by memory: 2,048 x 65,536 bf16
-// 87 us, 6.1 TB/s of reads (part of them still in the last-level cache) and writes.
+// 106 us, 5.1 TB/s of reads and writes; 86 right after the statistics, with part of the logits still in the last-level cache.
 template <class T, bool BY_ENTROPY, class How>
 __global__ __launch_bounds__(kRowThreads) void row_gradient_kernel(RowsIn in, GradIn g, How how) {
     constexpr int VEC = Chunk<T>::VEC;

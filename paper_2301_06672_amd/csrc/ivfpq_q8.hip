@@ -120,8 +120,8 @@ __device__ inline intx4 masked16(const int8_t* row, int at, int k) {
 // Few rows of a.  v_mfma_i32_16x16x64_i8: a wave has MT x NT blocks of 16 x 16; lane L brings row / column L % 16 and bytes
 // [16 (L / 16), ...) of each 64; register v of lane L holds row 4 (L / 16) + v, column L % 16.  The operands come straight
 // from memory in that layout (b is read once, a from the caches); the four waves of a workgroup take every fourth of the
-// 128-byte lines of the rows and add up through the LDS.  Bound by reading b: 32,768 rows of 4,096 against one row 24 us, 5.6 TB/s,
-// what a streaming read reaches.
+// 128-byte lines of the rows and add up through the LDS.  Bound by reading b: 32,768 rows of 4,096 against one row 24 us where
+// half of b is still in the last-level cache (two sets of weights in turn: 5.5 TB/s), 31 us where nothing is (eight in turn: 4.4 TB/s).
 template <class T, int MT, int NT>
 __global__ __launch_bounds__(256) void skinny_kernel(Product p) {
     __shared__ int sums[3][MT * NT * 4][64];
@@ -200,8 +200,8 @@ __global__ __launch_bounds__(256) void skinny_kernel(Product p) {
 // holds row 8 (v / 4) + 4 (L / 32) + v % 4, column L % 32.  Two rows of 128 bytes cover the 64 banks of the LDS, so the 16-byte
 // pieces of row r stand in the order piece ^ (r / 2 % 8): sixteen lanes that read one piece of sixteen rows use every bank
 // once.  Pieces are addressed by 32-bit offsets made once a tile (64-bit products for every load: 325 against 308 us below).
-// 2,048 x 32,768 bf16 results of 4,096 components: 272 us, 2.0 POP/s (the library's int8 product of that shape, without scales:
-// 264); 8,192^3 519 us, 2.1 POP/s (511).  The matrix cores are 0.4 busy; a CU's LDS reads (0.75 of the products' time), its loads of
+// 2,048 x 32,768 bf16 results of 4,096 components: 273 to 282 us, 2.0 POP/s (the library's int8 product of that shape, without scales:
+// 266 to 269); 8,192^3 484 us, 2.3 POP/s (440).  The matrix cores are 0.4 busy; a CU's LDS reads (0.75 of the products' time), its loads of
 // the next slice and the products overlap between the two waves of a SIMD, and all of them wait for the slowest at the barrier
 // of a slice.  Slices of 64 bytes, three of them ahead in four buffers: 343 against 308 us; slices begun at another place
 // by every workgroup, against rows a power of two apart in one channel: no gain (323 against 325).
@@ -226,7 +226,8 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     unsigned tile = blockIdx.x;
     // Rows of out that begin anywhere: the tiles of a row share the 64-byte pieces at their borders, which only one L2 can put
     // together.  Workgroups go to the eight XCDs in turn, so each XCD takes a range of consecutive tiles (777 x 100,003 fp32 results of 96
-    // components: 78 against 111 us).  Aligned rows pass the caches by instead (4,096 x 14,000, k = 256: 52 against 64 us).
+    // components: 78 against 111 us).  Aligned rows pass the caches by instead (2,048 x 32,768 bf16, k = 256: 77 against 85 us, k = 4,096: 268 against
+    // 277; 777 x 100,032 fp32, k = 96: 69 against 71; 4,096 x 14,016 fp32, k = 256: 66 and 65).
     if (!p.aligned) {
         const unsigned each = gridDim.x / 8, more = gridDim.x % 8, xcd = blockIdx.x % 8;
         tile = xcd * each + min(xcd, more) + blockIdx.x / 8;
