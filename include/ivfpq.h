@@ -373,6 +373,108 @@ int ivfpq_distill_topk_step(const void* d_logits, int32_t dtype, int64_t n, int3
                             const float* d_row_grads, float* d_loss, void* d_grad, int64_t grad_stride, void* d_workspace,
                             size_t workspace_bytes, void* hip_stream);
 
+/* ---- drafted tokens: from the neighbours' texts, through a paged cache, to the model's verdict ----
+ *
+ * The text behind a stored state goes on in some way; a neighbour's continuation is a draft of what the model will say.  One pass of the
+ * model then takes n sequences of m rows: row 0 the last token that was kept, the others drafts, each the successor of its parent row.
+ * ivfpq_neighbour_drafts makes these trees, ivfpq_cache_append and ivfpq_draft_attention take the rows through a layer,
+ * ivfpq_verify_drafts decides by the model's logits which rows are kept, and ivfpq_cache_keep closes the gaps between them in the caches.
+ *
+ *  - d_parents [n][m] int32: the row that a row follows, which comes before it; any value outside [0, row) marks a row that follows the
+ *    cache.  NULL: a chain, every row follows the one before it (row 0 the cache).  Trees have up to IVFPQ_MAX_DRAFT rows, chains
+ *    up to 2^20 where not stated otherwise (a prompt, or a piece of one).
+ *  - d_counts [n] int32: a sequence's used rows are the first of them (values outside [0, m] count as the nearest); NULL: all m.  Unused rows
+ *    change nothing in a cache, and nothing in them is read; what outputs hold for them is stated with each call.
+ *  - The cache of one layer: d_k_cache [n_pages][kv_heads][page][d] and d_v_cache [n_pages][kv_heads][page / 8][d][8], fp16 or bf16, 16-byte
+ *    aligned; values of 8 places lie side by side, so that a product over places reads 16 bytes of each component.  page: a power of two
+ *    from 16 to 256; d: a multiple of 8, 8 <= d <= 256.
+ *  - d_pages [n][max_pages] int32: place p of sequence s is place p % page of page d_pages[s][p / page].  d_lens [n] int32: places that
+ *    the sequence has in the cache before the pass (negative values count as 0); row i is at place lens + i.  A place beyond max_pages pages, or in a
+ *    page outside [0, n_pages), is not there: nothing is written to it and nothing read.  max_pages * page < 2^31 - 2^21.
+ *  - The pages that hold a pass's rows belong to one sequence only. */
+enum {
+    IVFPQ_MAX_DRAFT = 64,       /* rows of a tree */
+    IVFPQ_MAX_DRAFT_DEPTH = 15, /* tokens of a continuation */
+    IVFPQ_MAX_HEAD = 256        /* components of a head */
+};
+
+/* Search results as trees of drafted tokens.  Neighbour j continues with the tokens d_text[id], d_text[id + 1], ... (d_text [n_ids] int32: the
+ * token that followed each stored state, states in the order of their text), up to `depth` of them, to the end of d_text or to a negative
+ * token (the end of a document).  It weighs w_j = exp((d_min - d_j) / temperature), rounded to a multiple of 2^-32, d_min the smallest distance
+ * of those left in: a neighbour is left out where ivfpq_neighbour_tokens leaves it out.  A node of the tree is a beginning that
+ * continuations share and weighs the sum of theirs.  A query's tree is row 0 = d_last (the token that the query's state comes before), then the
+ * m - 1 heaviest nodes in descending order; of equal ones the shallower comes first, then the one whose first neighbour does.
+ *   d_tokens, d_parents, d_depths [nq][m] int32, d_logprobs [nq][m] fp32: a row's token, parent (-1: row 0), tokens since row 0, and the
+ *   logarithm of its share of the neighbours' weight (row 0: 0); rows behind the last node hold -1, -1, 0 and -inf.  d_counts [nq] int32: rows
+ *   of each tree, with row 0.
+ * 1 <= k <= IVFPQ_MAX_LISTED, 1 <= depth <= IVFPQ_MAX_DRAFT_DEPTH, 1 <= m <= IVFPQ_MAX_DRAFT, 1e-30 <= temperature <= 1e30. */
+int ivfpq_neighbour_drafts(const int64_t* d_ids, const float* d_dists, int64_t nq, int32_t k, const int32_t* d_text, int64_t n_ids,
+                           const int32_t* d_last, double temperature, int32_t depth, int32_t m, int32_t* d_tokens,
+                           int32_t* d_parents, int32_t* d_depths, float* d_logprobs, int32_t* d_counts, void* hip_stream);
+
+/* A layer's keys and values to their places in its cache, with the rotation of their positions; queries rotated alike.
+ *   d_k, d_v [n * m][kv_heads][d], d_q [n * m][heads][d] (may be NULL, then heads = 0 and d_q_out NULL) of `dtype`: any for a cache of either 16-bit
+ *   type if fp32, else the cache's own; k_stride, v_stride, q_stride values from one row to the next.
+ *   The position of a row is lens + d_depths[s][row] (d_depths [n][m] int32; NULL: lens + row).  The first `rotated` components of a head
+ *   are turned in pairs by position * d_inv_freq[i], i < rotated / 2, fp32: pairs (2i, 2i + 1) if interleaved, else (i, i + rotated / 2).  (a, b)
+ *   becomes amplitude * (a cos - b sin, b cos + a sin).  Frequencies scaled for long contexts, and the amplitude that goes with some of
+ *   them, are the caller's.  Angles are formed and reduced in 64 bits, the rest is fp32, rounded once to the cache's type.
+ *   0 <= rotated <= d, even; d_inv_freq may be NULL with rotated = 0.
+ *   d_q_out [n * m][heads][d] of the cache's type; zeros in unused rows. */
+int ivfpq_cache_append(const void* d_q, int64_t q_stride, int32_t heads, const void* d_k, int64_t k_stride, const void* d_v,
+                       int64_t v_stride, int32_t dtype, int64_t n, int32_t m, const int32_t* d_depths, const int32_t* d_counts,
+                       const float* d_inv_freq, int32_t rotated, int32_t interleaved, float amplitude, void* d_q_out, void* d_k_cache,
+                       void* d_v_cache, int32_t cache_dtype, int64_t n_pages, int32_t kv_heads, int32_t page, int32_t d,
+                       const int32_t* d_pages, int32_t max_pages, const int32_t* d_lens, void* hip_stream);
+
+/* Attention of the rows of a pass: row r of sequence s sees the lens[s] places of the cache before the pass, its ancestors among the rows, and
+ * itself, whose keys and values ivfpq_cache_append has put there:
+ *   out = sum_p softmax_p(scale * q . k_p) v_p,   lse = log sum_p exp(scale * q . k_p).
+ * What a row does not see has no influence on it, NaNs and infinities included.  A row that sees nothing (its places are not
+ * there) is 0 with lse = -inf; unused rows likewise.
+ *   d_q [n * m][heads][d] of the cache's type, 16-byte aligned, q_stride values from one row to the next, a multiple of 8; heads a multiple of kv_heads:
+ *   head h reads the keys and values of h / (heads / kv_heads).  d_out [n * m][heads][d] likewise, out_stride, 8-byte aligned.  d_lse [n * m][heads]
+ *   fp32, may be NULL.
+ *   max_places: no sequence has more places with its rows (later ones are not looked at); it decides how the work is divided only.
+ *   Probabilities are fp32; they are rounded to the cache's type as factors of the values (the sum that divides them is of unrounded ones).
+ * d_workspace: >= ivfpq_draft_attention_workspace_bytes(...) (may be 0), 256-byte aligned. */
+size_t ivfpq_draft_attention_workspace_bytes(int64_t n, int32_t m, int32_t heads, int32_t kv_heads, int32_t d, int64_t max_places);
+int ivfpq_draft_attention(const void* d_q, int64_t q_stride, int32_t heads, int64_t n, int32_t m, const int32_t* d_parents,
+                          const int32_t* d_counts, const void* d_k_cache, const void* d_v_cache, int32_t cache_dtype, int64_t n_pages,
+                          int32_t kv_heads, int32_t page, int32_t d, const int32_t* d_pages, int32_t max_pages, const int32_t* d_lens,
+                          int64_t max_places, float scale, void* d_out, int64_t out_stride, float* d_lse, void* d_workspace,
+                          size_t workspace_bytes, void* hip_stream);
+
+/* Which drafted tokens the model keeps, and what it says next.  Row i of sequence s has the logits in row s * m + i of d_logits, of the token behind
+ * it; p is their distribution at this temperature.  m <= IVFPQ_MAX_DRAFT, chains too.  From row 0 on:
+ *  - d_draft_logits NULL (drafts that were not drawn at random): the row's token is the lowest v with p_0 + ... + p_v > u, u = d_uniforms[s][i]
+ *    (d_uniforms [n][m] fp32; NULL: the most likely token, ties to the lowest).  If a used row that follows this one holds it (the first of them
+ *    that does), that row is kept and the next; otherwise it is the next token.
+ *  - d_draft_logits [n * (m - 1)][vocab] of the logits' type (a chain; d_uniforms and d_accept given): row s * (m - 1) + i holds the logits from
+ *    whose distribution q, at the same temperature, tokens[s][i + 1] was drawn.  Row i + 1 is kept if d_accept[s][i + 1] * q_x < p_x, x its token.
+ *    Otherwise the next token is drawn like above from max(p - q, 0) divided by its sum (from p if that is 0); behind
+ *    the last used row from p.  A row of draft logits without a distribution counts as q = 0.
+ * Either way what is said has the distribution of the model without drafts, if the random numbers are independent and uniform on [0, 1) (others count as
+ * the nearest number there, NaN as 0).  Sums are of 64 bits.
+ *   d_tokens [n][m] int32; d_tokens[s][0] is not looked at
+ *   d_path [n][m] int32: the kept rows, 0 first; then -1.  d_kept [n] int32: how many; 0 for a sequence without used rows.
+ *   d_next [n] int32: the token behind the last kept row; -1 without used rows, and where that row has no distribution or NaN statistics
+ *   d_logprobs [n][m] fp32: log p of the token behind each kept row (NaN in a row of NaN statistics); -inf in unused places.
+ * d_workspace: >= ivfpq_verify_drafts_workspace_bytes(...), 256-byte aligned; with_drafts: d_draft_logits is given. */
+size_t ivfpq_verify_drafts_workspace_bytes(int64_t n, int32_t m, int32_t vocab, int32_t with_drafts);
+int ivfpq_verify_drafts(const void* d_logits, int32_t dtype, int64_t n, int32_t m, int32_t vocab, int64_t row_stride,
+                        const int32_t* d_tokens, const int32_t* d_parents, const int32_t* d_counts, const float* d_uniforms,
+                        double temperature, const void* d_draft_logits, int64_t draft_stride, const float* d_accept, int32_t* d_path,
+                        int32_t* d_kept, int32_t* d_next, float* d_logprobs, void* d_workspace, size_t workspace_bytes,
+                        void* hip_stream);
+
+/* The kept rows move up behind each other: place lens + d_path[s][i] goes to lens + i, i < d_kept[s], in every layer.
+ * d_path [n][m] int32, ascending, d_kept [n] int32 as ivfpq_verify_drafts gives them: entries outside [i, m) move nothing.
+ * d_k_cache, d_v_cache: layers caches behind each other (all with the same pages).  The sequence's length is the caller's to raise by d_kept. */
+int ivfpq_cache_keep(void* d_k_cache, void* d_v_cache, int32_t cache_dtype, int32_t layers, int64_t n_pages, int32_t kv_heads, int32_t page,
+                     int32_t d, const int32_t* d_pages, int32_t max_pages, const int32_t* d_lens, int64_t n, int32_t m,
+                     const int32_t* d_path, const int32_t* d_kept, void* hip_stream);
+
 /* ---- measurement aid ---- */
 
 /* When enabled, search calls record HIP events around their stages on the stream they run on (the events

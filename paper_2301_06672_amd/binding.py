@@ -26,6 +26,7 @@ STATIC_SCRATCH_BYTES = 64 << 20
 TUNE_SCAN_THREADS, TUNE_ORDER_BLOCK, TUNE_SCAN_SHARE, TUNE_EARLY_EXIT, TUNE_LDS_PAD, TUNE_SCAN_ROUTE = 0, 1, 2, 3, 4, 5
 
 MAX_TOP, MAX_LISTED, MAX_MIXED, MAX_Q8_K = 128, 1024, 256, 65536
+MAX_DRAFT, MAX_DRAFT_DEPTH, MAX_HEAD = 64, 15, 256
 VALUES_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 OK, EINVAL, ENOSPACE, EHIP, EUNSUPPORTED, ESTATE = 0, -1, -2, -3, -4, -5
@@ -41,6 +42,8 @@ EXPORTS = (
     "ivfpq_quantize_rows", "ivfpq_q8_matmul", "ivfpq_neighbour_tokens", "ivfpq_token_logprobs_workspace_bytes",
     "ivfpq_token_logprobs", "ivfpq_token_logprobs_backward", "ivfpq_distill_topk_workspace_bytes", "ivfpq_distill_topk",
     "ivfpq_distill_topk_backward", "ivfpq_distill_topk_step",
+    "ivfpq_neighbour_drafts", "ivfpq_cache_append", "ivfpq_draft_attention_workspace_bytes", "ivfpq_draft_attention",
+    "ivfpq_verify_drafts_workspace_bytes", "ivfpq_verify_drafts", "ivfpq_cache_keep",
 )
 
 
@@ -117,6 +120,17 @@ def _declare(L):
     L.ivfpq_distill_topk.argtypes = logits + [vp, vp, i32, f32, vp, vp, vp, sz, vp]
     L.ivfpq_distill_topk_backward.argtypes = logits + [vp, vp, vp, i32, f32, vp, vp, i64, vp]
     L.ivfpq_distill_topk_step.argtypes = logits + [vp, vp, i32, f32, vp, vp, vp, i64, vp, sz, vp]
+    f64 = c.c_double
+    L.ivfpq_neighbour_drafts.argtypes = [vp, vp, i64, i32, vp, i64, vp, f64, i32, i32, vp, vp, vp, vp, vp, vp]
+    layout = [i64, i32, i32, i32, vp, i32, vp]
+    L.ivfpq_cache_append.argtypes = [vp, i64, i32, vp, i64, vp, i64, i32, i64, i32, vp, vp, vp, i32, i32, f32, vp, vp, vp, i32] + layout + [vp]
+    L.ivfpq_draft_attention_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64]
+    L.ivfpq_draft_attention_workspace_bytes.restype = sz
+    L.ivfpq_draft_attention.argtypes = [vp, i64, i32, i64, i32, vp, vp, vp, vp, i32] + layout + [i64, f32, vp, i64, vp, vp, sz, vp]
+    L.ivfpq_verify_drafts_workspace_bytes.argtypes = [i64, i32, i32, i32]
+    L.ivfpq_verify_drafts_workspace_bytes.restype = sz
+    L.ivfpq_verify_drafts.argtypes = [vp, i32, i64, i32, i32, i64, vp, vp, vp, vp, f64, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.ivfpq_cache_keep.argtypes = [vp, vp, i32, i32] + layout + [i64, i32, vp, vp, vp]
     L.ivfpq_last_error.restype = c.c_char_p
     for name in EXPORTS:
         fn = getattr(L, name)
@@ -418,6 +432,202 @@ def ivfpq_distill_topk_step(logits: torch.Tensor, teacher_tokens: torch.Tensor, 
     _check(lib().ivfpq_distill_topk_step(*_logits(x), _dp(tokens), _dp(values), tokens.shape[1], temperature, _dp(row_grads), _dp(loss),
                                          _dp(grad), grad.stride(0), _dp(ws), need, _stream()))
     return loss, grad
+
+
+# ---- drafted tokens.  n sequences of m rows a pass: row 0 the last token that was kept, the others drafts.
+
+class DraftTrees(NamedTuple):
+    tokens: torch.Tensor       # [n][m] int32; -1 behind a tree's rows
+    parents: torch.Tensor      # [n][m] int32: the row that each row follows; -1 for row 0
+    depths: torch.Tensor       # [n][m] int32: tokens since row 0
+    logprobs: torch.Tensor     # [n][m] fp32: of the way to a row, among the neighbours
+    counts: torch.Tensor       # [n] int32: rows of each tree
+
+
+class Verified(NamedTuple):
+    path: torch.Tensor         # [n][m] int32: the kept rows, then -1
+    kept: torch.Tensor         # [n] int32: how many
+    next_tokens: torch.Tensor  # [n] int32: the token behind the last kept row
+    logprobs: torch.Tensor     # [n][m] fp32: of the token behind each kept row
+
+
+def _optional(what: str, t: Optional[torch.Tensor], dtype, *shape):
+    return None if t is None else _plain(what, t, dtype, *shape)
+
+
+def _cache(what: str, k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.Tensor, lens: torch.Tensor, layers: bool = False):
+    """-> (layers, the arguments that describe a cache's layout, n, page, tensors that the call reads): caches are written or read in place, so they have to
+    be contiguous."""
+    if k_cache.dim() != 4 + layers or k_cache.dtype not in (torch.float16, torch.bfloat16):
+        _refuse(f"{what}: keys are float16 or bfloat16 {'[layers]' if layers else ''}[pages][heads][page][d], got {k_cache.dtype} {tuple(k_cache.shape)}")
+    *more, n_pages, kv_heads, page, d = k_cache.shape
+    if v_cache.dtype != k_cache.dtype or v_cache.shape != (*more, n_pages, kv_heads, page // 8, d, 8):
+        _refuse(f"{what}: values are {k_cache.dtype} {(*more, n_pages, kv_heads, page // 8, d, 8)}, got {v_cache.dtype} {tuple(v_cache.shape)}")
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous()):
+        _refuse(f"{what}: a cache is not contiguous")
+    if pages.dim() != 2 or lens.dim() != 1:
+        _refuse(f"{what}: pages are a matrix, lengths a vector")
+    n, most = pages.shape
+    for size in (kv_heads, page, d, most, *more):
+        _fits_int32(what, size)
+    pages, lens = _plain(what, pages, torch.int32, n, most), _plain(what, lens, torch.int32, n)
+    return (more[0] if layers else 1), (n_pages, kv_heads, page, d, _dp(pages), most, _dp(lens)), n, page, (pages, lens)
+
+
+def _head_rows(what: str, x: torch.Tensor, n: int, d: int, align: int = 1):
+    """-> (x, row stride): [n][m][heads][d] whose heads lie behind each other and whose rows lie a stride apart; other layouts are copied."""
+    if x.dim() != 4 or x.shape[0] != n or x.shape[3] != d:
+        _refuse(f"{what}: rows are [{n}][m][heads][{d}], got {tuple(x.shape)}")
+    _, m, heads, _ = x.shape
+    _fits_int32(what, m)
+    _fits_int32(what, heads)
+    if x.numel() == 0 or x.is_contiguous():
+        return x, heads * d
+    sn, sm, sh, sd = x.stride()
+    stride = sm if m > 1 else sn
+    fits = (sd == 1 or d == 1) and (sh == d or heads == 1) and (n == 1 or sn == m * stride) and stride >= heads * d and stride % align == 0
+    return (x, stride) if fits else (x.contiguous(), heads * d)
+
+
+def ivfpq_neighbour_drafts(ids: torch.Tensor, dists: torch.Tensor, text: torch.Tensor, last_tokens: torch.Tensor, temperature: float, depth: int = 8,
+                           rows: int = MAX_DRAFT) -> DraftTrees:
+    """Trees of `rows` rows from search results: text [n_ids] int32 is the token that followed each stored state, states in the order of their text."""
+    what = "ivfpq_neighbour_drafts"
+    _on_device(what, ids, dists, text, last_tokens)
+    if ids.dim() != 2:
+        _refuse(f"{what}: ids are a matrix")
+    nq, k = ids.shape
+    _fits_int32(what, k)
+    if not 1 <= depth <= MAX_DRAFT_DEPTH:
+        _refuse(f"{what}: depth={depth} outside [1, {MAX_DRAFT_DEPTH}]")
+    if not 1 <= rows <= MAX_DRAFT:
+        _refuse(f"{what}: rows={rows} outside [1, {MAX_DRAFT}]")
+    ids, dists = _plain(what, ids, torch.int64, nq, k), _plain(what, dists, torch.float32, nq, k)
+    text, last = _plain(what, text, torch.int32, text.numel()), _plain(what, last_tokens, torch.int32, nq)
+    three = torch.empty((3, nq, rows), dtype=torch.int32, device="cuda")
+    tokens, parents, depths = three[0], three[1], three[2]
+    logprobs = torch.empty((nq, rows), dtype=torch.float32, device="cuda")
+    counts = torch.empty(nq, dtype=torch.int32, device="cuda")
+    _check(lib().ivfpq_neighbour_drafts(_dp(ids), _dp(dists), nq, k, _dp(text), text.numel(), _dp(last), temperature, depth, rows, _dp(tokens), _dp(parents),
+                                        _dp(depths), _dp(logprobs), _dp(counts), _stream()))
+    return DraftTrees(tokens, parents, depths, logprobs, counts)
+
+
+def ivfpq_cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.Tensor, lens: torch.Tensor,
+                       q: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None, depths: Optional[torch.Tensor] = None,
+                       counts: Optional[torch.Tensor] = None, interleaved: bool = False, amplitude: float = 1.0) -> Optional[torch.Tensor]:
+    """Keys and values [n][m][heads][d] to their places, keys turned by their positions; -> the queries turned alike (None without q).  inv_freq [rotated / 2] fp32."""
+    what = "ivfpq_cache_append"
+    _on_device(what, k, v, k_cache, v_cache, pages, lens, q, inv_freq, depths, counts)
+    _, layout, n, _, held = _cache(what, k_cache, v_cache, pages, lens)
+    kv_heads, d = k_cache.shape[1], k_cache.shape[3]
+    if k.dtype not in VALUES_DTYPES or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+        _refuse(f"{what}: rows of {k.dtype} and {v.dtype}")
+    k, k_stride = _head_rows(what, k, n, d)
+    v, v_stride = _head_rows(what, v, n, d)
+    m = k.shape[1]
+    if k.shape != v.shape or k.shape[2] != kv_heads:
+        _refuse(f"{what}: keys {tuple(k.shape)} and values {tuple(v.shape)} for a cache of {kv_heads} heads")
+    heads, q_stride, turned = 0, 0, None
+    if q is not None:
+        q, q_stride = _head_rows(what, q, n, d)
+        if q.shape[1] != m or q.shape[2] < 1:
+            _refuse(f"{what}: queries {tuple(q.shape)} for {m} rows")
+        heads = q.shape[2]
+        turned = torch.empty(q.shape, dtype=k_cache.dtype, device="cuda")
+    half = 0 if inv_freq is None else inv_freq.numel()
+    _fits_int32(what, 2 * half)
+    inv_freq = _optional(what, inv_freq, torch.float32, half)
+    depths, counts = _optional(what, depths, torch.int32, n, m), _optional(what, counts, torch.int32, n)
+    _check(lib().ivfpq_cache_append(_dp(q), q_stride, heads, _dp(k), k_stride, _dp(v), v_stride, VALUES_DTYPES[k.dtype], n, m, _dp(depths), _dp(counts),
+                                    _dp(inv_freq), 2 * half, int(interleaved), amplitude, _dp(turned), _dp(k_cache), _dp(v_cache),
+                                    VALUES_DTYPES[k_cache.dtype], *layout, _stream()))
+    return turned
+
+
+def ivfpq_draft_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.Tensor, lens: torch.Tensor,
+                          parents: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                          max_places: Optional[int] = None, out: Optional[torch.Tensor] = None, with_lse: bool = False):
+    """-> [n][m][heads][d] (with_lse: and lse [n][m][heads] fp32): attention of a pass's rows over the cache, whose last m places hold theirs.
+    scale: d ** -0.5 if None.  max_places: what no sequence exceeds with its rows (all of `pages` if None), best close to the longest."""
+    what = "ivfpq_draft_attention"
+    _on_device(what, q, k_cache, v_cache, pages, lens, parents, counts, out)
+    _, layout, n, page, held = _cache(what, k_cache, v_cache, pages, lens)
+    kv_heads, d = k_cache.shape[1], k_cache.shape[3]
+    if q.dtype != k_cache.dtype:
+        _refuse(f"{what}: queries of {q.dtype} over a cache of {k_cache.dtype}")
+    q, q_stride = _head_rows(what, q, n, d, 8)
+    if q.data_ptr() % 16:
+        q, q_stride = q.clone(memory_format=torch.contiguous_format), q.shape[2] * d
+    m, heads = q.shape[1], q.shape[2]
+    if m < 1 or heads < 1:
+        _refuse(f"{what}: queries {tuple(q.shape)}")
+    parents, counts = _optional(what, parents, torch.int32, n, m), _optional(what, counts, torch.int32, n)
+    if out is None:
+        out = torch.empty((n, m, heads, d), dtype=q.dtype, device="cuda")
+    if out.shape != (n, m, heads, d) or out.dtype != q.dtype or not out.is_contiguous():
+        _refuse(f"{what}: out has another shape, type or layout than the queries")
+    lse = torch.empty((n, m, heads), dtype=torch.float32, device="cuda") if with_lse else None
+    if max_places is None:
+        max_places = pages.shape[1] * page
+    if not 0 <= max_places < 2 ** 62:
+        _refuse(f"{what}: max_places={max_places}")
+    need = lib().ivfpq_draft_attention_workspace_bytes(n, m, heads, kv_heads, d, max_places)
+    ws = _scratch(need)
+    _check(lib().ivfpq_draft_attention(_dp(q), q_stride, heads, n, m, _dp(parents), _dp(counts), _dp(k_cache), _dp(v_cache), VALUES_DTYPES[q.dtype], *layout,
+                                       max_places, d ** -0.5 if scale is None else scale, _dp(out), heads * d, _dp(lse), _dp(ws), need, _stream()))
+    return (out, lse) if with_lse else out
+
+
+def ivfpq_verify_drafts(logits: torch.Tensor, tokens: torch.Tensor, parents: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None,
+                        uniforms: Optional[torch.Tensor] = None, temperature: float = 1.0, draft_logits: Optional[torch.Tensor] = None,
+                        accept: Optional[torch.Tensor] = None) -> Verified:
+    """Which rows of tokens [n][m] the model's logits [n * m][vocab] keep, and the token behind them.  uniforms [n][m]: where in its distribution each row's
+    token is (None: the most likely one).  draft_logits [n * (m - 1)][vocab] and accept [n][m]: for drafts that were drawn from a student's distribution."""
+    what = "ivfpq_verify_drafts"
+    _on_device(what, logits, tokens, parents, counts, uniforms, draft_logits, accept)
+    x = _value_rows(what, logits)
+    if tokens.dim() != 2:
+        _refuse(f"{what}: tokens are a matrix")
+    n, m = tokens.shape
+    _fits_int32(what, m)
+    if x.shape[0] != n * m:
+        _refuse(f"{what}: {x.shape[0]} rows of logits for {n} x {m} tokens")
+    tokens, parents, counts = _plain(what, tokens, torch.int32, n, m), _optional(what, parents, torch.int32, n, m), _optional(what, counts, torch.int32, n)
+    uniforms, accept = _optional(what, uniforms, torch.float32, n, m), _optional(what, accept, torch.float32, n, m)
+    if draft_logits is not None:
+        drafts = _value_rows(what, draft_logits)
+        if drafts.shape != (n * (m - 1), x.shape[1]) or drafts.dtype != x.dtype:
+            _refuse(f"{what}: draft logits {drafts.dtype} {tuple(drafts.shape)} for {n} x {m} tokens")
+        if uniforms is None or accept is None:
+            _refuse(f"{what}: drafts that were drawn need both random numbers")
+        if m <= 1:
+            draft_logits = None                            # nothing was drafted
+    if draft_logits is None:
+        drafts = None
+    path = torch.empty((n, m), dtype=torch.int32, device="cuda")
+    logprobs = torch.empty((n, m), dtype=torch.float32, device="cuda")
+    kept, following = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(n, dtype=torch.int32, device="cuda")
+    need = lib().ivfpq_verify_drafts_workspace_bytes(n, m, x.shape[1], drafts is not None)
+    ws = _scratch(need)
+    _check(lib().ivfpq_verify_drafts(_dp(x), VALUES_DTYPES[x.dtype], n, m, x.shape[1], x.stride(0), _dp(tokens), _dp(parents), _dp(counts), _dp(uniforms),
+                                     temperature, _dp(drafts), 0 if drafts is None else drafts.stride(0), _dp(accept), _dp(path), _dp(kept),
+                                     _dp(following), _dp(logprobs), _dp(ws), need, _stream()))
+    return Verified(path, kept, following, logprobs)
+
+
+def ivfpq_cache_keep(k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.Tensor, lens: torch.Tensor, path: torch.Tensor, kept: torch.Tensor):
+    """The kept rows (path, kept of Verified) move up behind each other in the caches [layers][pages][heads][page][d] (values [layers][pages][heads][page / 8][d][8];
+    one layer's without the first dimension); raise `lens` by `kept` afterwards."""
+    what = "ivfpq_cache_keep"
+    _on_device(what, k_cache, v_cache, pages, lens, path, kept)
+    layers, layout, n, _, held = _cache(what, k_cache, v_cache, pages, lens, layers=k_cache.dim() == 5)
+    if path.dim() != 2:
+        _refuse(f"{what}: paths are a matrix")
+    m = path.shape[1]
+    _fits_int32(what, m)
+    path, kept = _plain(what, path, torch.int32, n, m), _plain(what, kept, torch.int32, n)
+    _check(lib().ivfpq_cache_keep(_dp(k_cache), _dp(v_cache), VALUES_DTYPES[k_cache.dtype], layers, *layout, n, m, _dp(path), _dp(kept), _stream()))
 
 
 class Index:

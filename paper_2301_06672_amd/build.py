@@ -23,9 +23,12 @@ HIP_FLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 # (object, source, flags): search, the matrix-core filter of its scan and the sums of what that lists, the scan of groups of
-# pairs (one object per table dtype each), index construction; log-probabilities and distillation, neighbours' tokens, 8-bit products
+# pairs (one object per table dtype each), index construction; log-probabilities and distillation, neighbours' tokens, 8-bit products; drafted
+# tokens: trees, caches, attention, verification
 DEVICE_OBJECTS = [("ivfpq_device", "ivfpq_device", []), ("ivfpq_build", "ivfpq_build", []), ("ivfpq_scan_filter", "ivfpq_scan_filter", []),
                   ("ivfpq_logits", "ivfpq_logits", []), ("ivfpq_neighbours", "ivfpq_neighbours", []), ("ivfpq_q8", "ivfpq_q8", []),
+                  ("ivfpq_drafts", "ivfpq_drafts", []), ("ivfpq_cache", "ivfpq_cache", []), ("ivfpq_attention", "ivfpq_attention", []),
+                  ("ivfpq_verify", "ivfpq_verify", []),
                   *((f"ivfpq_candidates_{lut}", "ivfpq_candidates", [f"-DIVFPQ_CANDIDATE_LUT={lut}"]) for lut in range(4)),
                   *((f"ivfpq_scan_group_{lut}", "ivfpq_scan_group", [f"-DIVFPQ_GROUP_LUT={lut}"]) for lut in range(4))]
 HOST_FLAGS = ["-O3", "-std=c++17", "-fPIC", "-fopenmp", "-mavx2", "-mfma", "-Wall"]

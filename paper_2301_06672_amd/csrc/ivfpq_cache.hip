@@ -1,0 +1,308 @@
+// A paged cache of keys and values: rows of a pass rotated and put to their places (ivfpq_cache_append), the kept ones moved
+// up behind each other (ivfpq_cache_keep).
+//
+// A pair (a, b) of components at position p turns by p f: amplitude (a cos - b sin, b cos + a sin).  p f is a product of 64 bits, and
+// what is left of it modulo 2 pi fits 32: an angle of 10^6 would be off by 0.03 in fp32.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "ivfpq_cache.hpp"
+
+using namespace ivfpq;
+
+namespace {
+
+struct AppendIn {
+    const void *q, *k, *v;
+    long long q_stride, k_stride, v_stride;
+    void *q_out, *k_cache, *v_cache;
+    const int* depths;                // [n][m] or null
+    const float* inv_freq;            // [rotated / 2]
+    int heads, rotated, interleaved, granules;
+    bool q_pieces, k_pieces, v_pieces; // rows are 16-byte aligned
+    float amplitude;
+    Pages at;
+};
+
+// 8 consecutive values of a row, widened
+template <class T>
+__device__ inline void load8(const T* p, bool pieces, float (&x)[8]) {
+    if (pieces) {
+        constexpr int VEC = Chunk<T>::VEC;
+#pragma unroll
+        for (int i = 0; i < 8 / VEC; ++i) {
+            Chunk<T> c;
+            c.bits = reinterpret_cast<const uint4*>(p)[i];
+            float part[VEC];
+            c.widen(part);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) x[i * VEC + j] = part[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (float)p[i];
+    }
+}
+
+constexpr int kAppendThreads = 256;
+
+// One workgroup for the rows whose places are one granule of 8: their values go to the cache as whole 16-byte pieces, and an angle is
+// formed once for all heads.  Bound by HBM with prompts, by latency with single tokens.
+template <class T, class C>
+__global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendIn in) {
+    __shared__ float turns[8][kMostHead];           // cos, then sin, of each pair
+    const int tid = threadIdx.x, d = in.at.d, m = in.at.m, kv_heads = in.at.kv_heads;
+    const long long s = blockIdx.x / in.granules;
+    const int len = in.at.len(s), count = in.at.count(s);
+    const long long granule = (len >> 3) + (long long)(blockIdx.x % in.granules);
+    // rows [first, last) of the granule's places; place 8 * granule + i holds row base + i
+    const long long base = granule * 8 - len;
+    const int first = (int)max(base, 0ll), used = (int)min(base + 8, (long long)count), all = (int)min(base + 8, (long long)m);
+    if (first >= all) return;
+    const int half = in.rotated / 2;
+    for (int i = tid; i < (used - first) * half; i += kAppendThreads) {
+        const int row = first + i / half, pair = i % half;
+        const double position = (double)len + (double)(in.depths ? in.depths[s * m + row] : row);
+        double turn = position * (double)in.inv_freq[pair] * 0.15915494309189535;           // of 2 pi
+        turn -= rint(turn);
+        float sine, cosine;
+        sincosf((float)(turn * 6.283185307179586), &sine, &cosine);
+        turns[row - base][pair] = cosine * in.amplitude;
+        turns[row - base][half + pair] = sine * in.amplitude;
+    }
+    __syncthreads();
+
+    const int pieces = d / 8;                       // of a head
+    const int page = used > first ? in.at.page_of(s, granule * 8) : -1;
+    const int off = (int)(granule * 8) & (in.at.page() - 1);
+    C* k_page = (C*)in.k_cache + (page < 0 ? 0 : page) * in.at.page_values();
+    C* v_page = (C*)in.v_cache + (page < 0 ? 0 : page) * in.at.page_values();
+
+    // queries, then keys: a piece of 8 components a thread
+    const int per_row = (in.heads + kv_heads) * pieces;
+    for (int i = tid; i < (all - first) * per_row; i += kAppendThreads) {
+        const int row = first + i / per_row, piece = i % per_row;
+        const int head = piece / pieces, c = piece % pieces * 8;
+        const bool query = head < in.heads;
+        const long long flat = s * m + row;
+        typedef C out_t __attribute__((ext_vector_type(8)));
+        out_t y;
+        if (row >= used) {
+            if (!query) continue;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = (C)0.f;
+        } else {
+            if (!query && page < 0) continue;
+            const bool whole = query ? in.q_pieces : in.k_pieces;
+            const T* x = query ? (const T*)in.q + flat * in.q_stride + (long long)head * d : (const T*)in.k + flat * in.k_stride + (long long)(head - in.heads) * d;
+            const float* turn = turns[row - base];
+            float a[8], b[8];
+            load8(x + c, whole, a);
+            if (c >= in.rotated) {
+            } else if (in.interleaved) {
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    const int pair = (c + j) / 2;
+                    if (c + j < in.rotated) {
+                        const float cosine = turn[pair], sine = turn[half + pair], p = a[j], r = a[j + 1];
+                        a[j] = p * cosine - r * sine;
+                        a[j + 1] = r * cosine + p * sine;
+                    }
+                }
+            } else if (half % 8 == 0) {
+                const bool low = c < half;
+                load8(x + (low ? c + half : c - half), whole, b);
+                const float* cosine = turn + (low ? c : c - half);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) a[j] = low ? a[j] * cosine[j] - b[j] * cosine[half + j] : a[j] * cosine[j] + b[j] * cosine[half + j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int e = c + j;
+                    if (e >= in.rotated) continue;
+                    const int pair = e < half ? e : e - half;
+                    const float other = (float)x[e < half ? e + half : e - half], cosine = turn[pair], sine = turn[half + pair];
+                    a[j] = e < half ? a[j] * cosine - other * sine : a[j] * cosine + other * sine;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = (C)a[j];
+        }
+        C* to = query ? (C*)in.q_out + (flat * in.heads + head) * d + c : k_page + (((long long)(head - in.heads) << in.at.shift) + off + (row - base)) * d + c;
+        *reinterpret_cast<out_t*>(to) = y;
+    }
+
+    // values: 8 components of the granule's rows a thread, turned over in registers
+    if (page < 0) return;
+    for (int i = tid; i < kv_heads * pieces; i += kAppendThreads) {
+        const int head = i / pieces, c = i % pieces * 8;
+        C* to = v_page + (((long long)head << in.at.shift) + off) * d + c * 8;
+        const T* x = (const T*)in.v + (s * m + base) * in.v_stride + (long long)head * d + c;
+        if (used - first == 8) {
+            C held[8][8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                float a[8];
+                load8(x + r * in.v_stride, in.v_pieces, a);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) held[j][r] = (C)a[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                typedef C out_t __attribute__((ext_vector_type(8)));
+                out_t y;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) y[r] = held[j][r];
+                *reinterpret_cast<out_t*>(to + j * 8) = y;
+            }
+        } else {
+            for (int row = first; row < used; ++row) {
+                float a[8];
+                load8(x + (row - base) * in.v_stride, in.v_pieces, a);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) to[j * 8 + (row - base)] = (C)a[j];
+            }
+        }
+    }
+}
+
+struct KeepIn {
+    uint16_t *k_cache, *v_cache;
+    const int *path, *kept;           // [n][m], [n]
+    int layers;
+    Pages at;
+};
+
+constexpr int kKeepThreads = 256, kKeepBatch = 8;
+
+// A thread moves 8 components of a head through all kept rows.  The row that comes to place i lies at i or behind it and before the sources of later
+// places, so what a batch overwrites is never read by a later one; within a batch everything is read first.
+__global__ __launch_bounds__(kKeepThreads) void cache_keep_kernel(KeepIn in) {
+    const int d = in.at.d, m = in.at.m, pieces = d / 8, per = in.at.kv_heads * pieces;
+    const long long s = blockIdx.y;
+    const int kept = min(max(in.kept[s], 0), m);
+    const long long len = in.at.len(s);
+    const long long i = (long long)blockIdx.x * kKeepThreads + threadIdx.x;
+    if (i >= (long long)per * in.layers) return;
+    const long long layer = i / per;
+    const int head = (int)(i % per) / pieces, c = (int)(i % per) % pieces * 8;
+    uint16_t* k = in.k_cache + layer * in.at.n_pages * in.at.page_values();
+    uint16_t* v = in.v_cache + layer * in.at.n_pages * in.at.page_values();
+    const int* path = in.path + s * m;
+    const long long head_base = (long long)head << in.at.shift;
+    const int in_page = in.at.page() - 1;
+    for (int at = 0; at < kept; at += kKeepBatch) {
+        uint4 keys[kKeepBatch];
+        uint16_t values[kKeepBatch][8];
+        int target[kKeepBatch];                      // the page of the place it goes to, -1: nothing moves
+#pragma unroll
+        for (int j = 0; j < kKeepBatch; ++j) {
+            target[j] = -1;
+            if (at + j >= kept) continue;
+            const int row = path[at + j];
+            if (row <= at + j || row >= m) continue; // in place already, or no row of the pass
+            const int page = in.at.page_of(s, len + row);
+            if (page < 0) continue;
+            target[j] = in.at.page_of(s, len + at + j);
+            if (target[j] < 0) continue;
+            const int off = (int)(len + row) & in_page;
+            const long long from = (long long)page * in.at.page_values();
+            keys[j] = *reinterpret_cast<const uint4*>(k + from + (head_base + off) * d + c);
+            const uint16_t* x = v + from + (head_base + (off & ~7)) * d + c * 8 + (off & 7);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) values[j][e] = x[e * 8];
+        }
+#pragma unroll
+        for (int j = 0; j < kKeepBatch; ++j) {
+            if (target[j] < 0) continue;
+            const int off = (int)(len + at + j) & in_page;
+            const long long to = (long long)target[j] * in.at.page_values();
+            *reinterpret_cast<uint4*>(k + to + (head_base + off) * d + c) = keys[j];
+            uint16_t* y = v + to + (head_base + (off & ~7)) * d + c * 8 + (off & 7);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e * 8] = values[j][e];
+        }
+    }
+}
+
+template <class T, class C>
+int launch_append(const AppendIn& in, int64_t n, hipStream_t stream) {
+    hipLaunchKernelGGL((cache_append_kernel<T, C>), dim3((unsigned)(n * in.granules)), dim3(kAppendThreads), 0, stream, in);
+    HIP_TRY(hipGetLastError());
+    return IVFPQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ivfpq_cache_append(const void* d_q, int64_t q_stride, int32_t heads, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride,
+                       int32_t dtype, int64_t n, int32_t m, const int32_t* d_depths, const int32_t* d_counts, const float* d_inv_freq,
+                       int32_t rotated, int32_t interleaved, float amplitude, void* d_q_out, void* d_k_cache, void* d_v_cache,
+                       int32_t cache_dtype, int64_t n_pages, int32_t kv_heads, int32_t page, int32_t d, const int32_t* d_pages,
+                       int32_t max_pages, const int32_t* d_lens, void* hip_stream) {
+    return guarded("ivfpq_cache_append", [&] {
+        const char* what = "ivfpq_cache_append";
+        if (int rc = check_cache(what, d_k_cache, d_v_cache, cache_dtype, n_pages, kv_heads, page, d, d_pages, max_pages, d_lens, n, m)) return rc;
+        if (!known_dtype(dtype)) return fail(IVFPQ_EINVAL, "%s: unknown dtype %d", what, dtype);
+        if (dtype != IVFPQ_VALUES_FP32 && dtype != cache_dtype) return fail(IVFPQ_EINVAL, "%s: 16-bit rows are of the cache's dtype", what);
+        if (m > kMostChain) return fail(IVFPQ_EUNSUPPORTED, "%s: m=%d (limit 2^20 rows)", what, m);
+        if (heads < 0 || (heads > 0) != (d_q != nullptr) || (heads > 0) != (d_q_out != nullptr))
+            return fail(IVFPQ_EINVAL, "%s: heads, queries and their output come together", what);
+        if (heads > 65536) return fail(IVFPQ_EUNSUPPORTED, "%s: heads=%d (limit 65536)", what, heads);
+        if (rotated < 0 || rotated > d || rotated % 2) return fail(IVFPQ_EINVAL, "%s: rotated=%d is no even number up to d=%d", what, rotated, d);
+        if (n == 0) return (int)IVFPQ_OK;
+        if (!d_k || !d_v || (rotated > 0 && !d_inv_freq)) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
+        const int64_t rows = n * m, vb = value_bytes(dtype);
+        if (rows > 1 && (k_stride < (int64_t)kv_heads * d || v_stride < (int64_t)kv_heads * d || (heads && q_stride < (int64_t)heads * d)))
+            return fail(IVFPQ_EINVAL, "%s: a row stride below the row's values", what);
+        if ((uintptr_t)d_k % vb || (uintptr_t)d_v % vb || (uintptr_t)d_q % vb || (uintptr_t)d_q_out % 16)
+            return fail(IVFPQ_EINVAL, "%s: rows are not aligned to their type, or the queries' output not to 16 bytes", what);
+        const auto whole = [&](const void* p, int64_t stride) { return (uintptr_t)p % 16 == 0 && (rows == 1 || stride * vb % 16 == 0); };
+        AppendIn in{d_q, d_k, d_v, q_stride, k_stride, v_stride, d_q_out, d_k_cache, d_v_cache, d_depths, d_inv_freq, heads, rotated, interleaved,
+                    (int)(((int64_t)m + 7 + 7) / 8),           // a pass may begin inside of a granule
+                    whole(d_q, q_stride), whole(d_k, k_stride), whole(d_v, v_stride), amplitude,
+                    pages_in(d_pages, max_pages, d_lens, d_counts, n_pages, kv_heads, page, d, m)};
+        if (m == 1) in.granules = 1;
+        const hipStream_t stream = (hipStream_t)hip_stream;
+        return with_value_type(dtype, [&](auto t) {
+            using T = decltype(t);
+            if (cache_dtype == IVFPQ_VALUES_FP16) {
+                if constexpr (!std::is_same<T, bf16_t>::value) return launch_append<T, half_t>(in, n, stream);
+            } else {
+                if constexpr (!std::is_same<T, half_t>::value) return launch_append<T, bf16_t>(in, n, stream);
+            }
+            return (int)IVFPQ_EINVAL;
+        });
+    });
+}
+
+int ivfpq_cache_keep(void* d_k_cache, void* d_v_cache, int32_t cache_dtype, int32_t layers, int64_t n_pages, int32_t kv_heads, int32_t page,
+                     int32_t d, const int32_t* d_pages, int32_t max_pages, const int32_t* d_lens, int64_t n, int32_t m, const int32_t* d_path,
+                     const int32_t* d_kept, void* hip_stream) {
+    return guarded("ivfpq_cache_keep", [&] {
+        const char* what = "ivfpq_cache_keep";
+        if (int rc = check_cache(what, d_k_cache, d_v_cache, cache_dtype, n_pages, kv_heads, page, d, d_pages, max_pages, d_lens, n, m)) return rc;
+        if (layers < 1 || layers > 4096) return fail(IVFPQ_EINVAL, "%s: layers=%d outside [1, 4096]", what, layers);
+        if (m > kMostChain) return fail(IVFPQ_EUNSUPPORTED, "%s: m=%d (limit 2^20 rows)", what, m);
+        if (n == 0) return (int)IVFPQ_OK;
+        if (!d_path || !d_kept) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
+        const KeepIn whole{(uint16_t*)d_k_cache, (uint16_t*)d_v_cache, d_path, d_kept, layers, pages_in(d_pages, max_pages, d_lens, nullptr, n_pages, kv_heads, page, d, m)};
+        const int64_t items = (int64_t)layers * kv_heads * (d / 8);
+        constexpr int64_t kPiece = 32768;                  // sequences of a launch
+        for (int64_t at = 0; at < n; at += kPiece) {
+            KeepIn in = whole;
+            in.path += at * m;
+            in.kept += at;
+            in.at.lens += at;
+            in.at.pages += at * max_pages;
+            hipLaunchKernelGGL(cache_keep_kernel, dim3((unsigned)((items + kKeepThreads - 1) / kKeepThreads), (unsigned)std::min(kPiece, n - at)),
+                               dim3(kKeepThreads), 0, (hipStream_t)hip_stream, in);
+            HIP_TRY(hipGetLastError());
+        }
+        return (int)IVFPQ_OK;
+    });
+}
+
+}  // extern "C"

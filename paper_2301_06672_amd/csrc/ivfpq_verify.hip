@@ -1,0 +1,590 @@
+// Drafted tokens against the model's logits: what ivfpq_verify_drafts does.
+//
+// A token is drawn by where a given number falls among sums of probabilities, and as many borders as there are tokens lie close together, so sums are of
+// 64 bits and their terms right to 10^-12: 2^y = 2^n 2^f with n the nearest whole number and a polynomial of degree 8 for 2^f, |f| <= 1/2
+// (interpolated at Chebyshev's points, off by 1.1 10^-12 at most).  A row is read once, in blocks whose largest logit and sum about it
+// are kept; where a token is drawn, the sums say in which block, and that block is read again.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "ivfpq_values.hpp"
+
+using namespace ivfpq;
+
+namespace {
+
+constexpr int kMostDraft = IVFPQ_MAX_DRAFT;
+constexpr int kBlock = 2048;                          // values of a block, one wave's work: 32 a lane
+constexpr int kLaneValues = kBlock / 64;
+
+// What is kept of a block: the sum of exp((x - most) / T).  NaN and +inf stay in `most`.
+struct BlockSum {
+    double sum;
+    float most;
+    int unused;
+};
+
+struct VerifyIn {
+    const void *logits, *drafts;
+    long long stride, draft_stride;
+    const int *tokens, *parents, *counts;             // [n][m]; parents, counts or null
+    const float *uniforms, *accept;                   // [n][m] or null
+    BlockSum* blocks;                                 // [n * m + n * (m - 1) with drafts][row_blocks]
+    double* left;                                     // drafts: [n][left_blocks]
+    struct Stop* stops;                               // drafts: [n]
+    int *path, *kept, *next;
+    float* logprobs;
+    long long n;
+    int m, vocab, row_blocks, left_blocks;
+    double scale;                                     // log2(e) / T
+    __device__ inline int count(long long s) const { return counts ? min(max(counts[s], 0), m) : m; }
+};
+
+// Where a sequence's chain ends: the row whose distribution the next token comes from, and what normalises it and its draft's.
+struct Stop {
+    float most, draft_most;
+    double total, draft_total;                        // 0: no distribution
+    int row, drafted;                                 // row -1: no used rows; drafted: less the draft's probabilities
+};
+
+__device__ inline float maximum3(float a, float b, float c) {       // NaN if one of them is
+    float d;
+    asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    return d;
+}
+
+// 2^y for y <= 0, right to 1.1 10^-12; what is under 2^-1000 may be anything down to 0
+__device__ inline double exp2_exact(double y) {
+    y = fmax(y, -1100.0);
+    const double n = rint(y), f = y - n;
+    double p = 0x1.63d1363a7ecb6p-20;
+    p = fma(p, f, 0x1.00dc4a534054dp-16);
+    p = fma(p, f, 0x1.4308ac85a6c21p-13);
+    p = fma(p, f, 0x1.5d8745a72827ap-10);
+    p = fma(p, f, 0x1.3b2ab7181b778p-7);
+    p = fma(p, f, 0x1.c6b08dd6fd236p-5);
+    p = fma(p, f, 0x1.ebfbdff823cedp-3);
+    p = fma(p, f, 0x1.62e42fef84cf0p-1);
+    p = fma(p, f, 1.0);
+    return __builtin_amdgcn_ldexp(p, (int)n);
+}
+// exp((x - most) / T); `most` is finite
+__device__ inline double weight(float x, float most, double scale) { return exp2_exact(((double)x - (double)most) * scale); }
+
+__device__ inline double wave_sum(double x) {
+    for (int off = 32; off; off >>= 1) x += __shfl_xor(x, off);
+    return x;
+}
+// the sum over the lanes up to this one
+__device__ inline double wave_scan(double x) {
+    for (int off = 1; off < 64; off <<= 1) {
+        const double below = __shfl_up(x, off);
+        if ((int)(threadIdx.x & 63) >= off) x += below;
+    }
+    return x;
+}
+__device__ inline bool bad_most(float most) { return !(most < INFINITY); }       // NaN or +inf in the row
+
+// A block of a row as the wave's chunks: chunk i * 64 + lane holds VEC consecutive values, -inf outside of the row.
+template <class T>
+struct BlockChunks {
+    static constexpr int N = kLaneValues / Chunk<T>::VEC;
+    Chunk<T> chunk[N];
+    __device__ BlockChunks(const RowChunks<T>& row, int block, int lane) {
+        const int first = block * (kBlock / Chunk<T>::VEC);
+        if (first >= row.first_whole() && first + N * 64 <= row.end_whole()) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) chunk[i].bits = row.base[first + i * 64 + lane];
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int c = first + i * 64 + lane;
+                if (c < row.count()) chunk[i] = row.load(c);
+                else {
+                    float none[Chunk<T>::VEC];
+#pragma unroll
+                    for (int e = 0; e < Chunk<T>::VEC; ++e) none[e] = -INFINITY;
+                    chunk[i].narrow(none);
+                }
+            }
+        }
+    }
+};
+
+constexpr int kSumThreads = 256;
+
+// The blocks' sums of all used rows, a wave a block.  Bound by 64-bit arithmetic: some 18 operations a value.
+template <class T>
+__global__ __launch_bounds__(kSumThreads) void block_sums_kernel(VerifyIn in) {
+    constexpr int VEC = Chunk<T>::VEC;
+    const int lane = threadIdx.x & 63;
+    const long long item = (long long)blockIdx.x * (kSumThreads / 64) + (threadIdx.x >> 6);
+    const long long row = item / in.row_blocks, targets = in.n * in.m;
+    const int block = (int)(item % in.row_blocks);
+    const bool draft = row >= targets;
+    const long long r = draft ? row - targets : row;
+    if (draft && (!in.drafts || r >= in.n * (in.m - 1))) return;
+    const int per = draft ? in.m - 1 : in.m;
+    // a draft row is used if the row that it drafted is
+    if ((int)(r % per) + (draft ? 1 : 0) >= in.count(r / per)) return;
+    const RowChunks<T> values(draft ? in.drafts : in.logits, r, draft ? in.draft_stride : in.stride, in.vocab);
+    if (block * kBlock >= values.end) return;
+    BlockChunks<T> held(values, block, lane);
+    float most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < held.N; ++i) {
+        float x[VEC];
+        held.chunk[i].widen(x);
+#pragma unroll
+        for (int e = 0; e < VEC; e += 2) most = maximum3(most, x[e], x[e + 1]);
+        held.chunk[i].forget_widened();
+    }
+    for (int off = 32; off; off >>= 1) {
+        const float other = __shfl_xor(most, off);
+        most = maximum3(most, other, other);
+    }
+    double sum = 0.0;
+    if (most > -INFINITY && most < INFINITY) {
+#pragma unroll
+        for (int i = 0; i < held.N; ++i) {
+            float x[VEC];
+            held.chunk[i].widen(x);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum += weight(x[e], most, in.scale);
+        }
+        sum = wave_sum(sum);
+    }
+    if (lane == 0) in.blocks[row * in.row_blocks + block] = BlockSum{sum, most, 0};
+}
+
+// A row's largest logit and the sum about it, from its blocks; the same in every lane.
+struct Norm {
+    float most;
+    double total;                                     // 0: all -inf; NaN: bad
+};
+__device__ inline Norm row_norm(const BlockSum* blocks, int count, double scale, int lane) {
+    float most = -INFINITY;
+    for (int b = lane; b < count; b += 64) most = maximum3(most, blocks[b].most, blocks[b].most);
+    for (int off = 32; off; off >>= 1) {
+        const float other = __shfl_xor(most, off);
+        most = maximum3(most, other, other);
+    }
+    if (bad_most(most)) return Norm{most, NAN};
+    if (most == -INFINITY) return Norm{most, 0.0};
+    double total = 0.0;
+    for (int b = lane; b < count; b += 64)
+        if (blocks[b].most > -INFINITY) total += blocks[b].sum * weight(blocks[b].most, most, scale);
+    return Norm{most, wave_sum(total)};
+}
+
+__device__ inline double unit(float u) {              // into [0, 1)
+    return (double)fminf(fmaxf(u, 0.f), 0x1.fffffep-1f);
+}
+
+// The first block of `count` whose running sum, `of` it, is over `share` times the sum of all; `before`: the sum of those before it.  -1 if all are 0.
+template <class Of>
+__device__ inline int pick_block(int count, double share, int lane, double& before, Of&& of, double& all) {
+    all = 0.0;
+    for (int b = lane; b < count; b += 64) all += of(b);
+    all = wave_sum(all);
+    if (!(all > 0.0)) return -1;
+    const double target = share * all;
+    double base = 0.0;
+    int last = -1;                                    // the last block that is not 0: what rounding may leave over falls there
+    double last_base = 0.0;
+    for (int first = 0; first < count; first += 64) {
+        const int b = first + lane;
+        const double mine = b < count ? of(b) : 0.0;
+        const double upto = base + wave_scan(mine);
+        const uint64_t over = __ballot(mine > 0.0 && upto > target);
+        const uint64_t some = __ballot(mine > 0.0);
+        if (over) {
+            const int l = __ffsll((unsigned long long)over) - 1;
+            before = l ? __shfl(upto, l - 1) : base;
+            return first + l;
+        }
+        if (some) {
+            const int l = 63 - __clzll((long long)some);
+            last = first + l;
+            last_base = l ? __shfl(upto, l - 1) : base;
+        }
+        base = __shfl(upto, 63);
+    }
+    before = last_base;
+    return last;
+}
+
+// The lowest token of a block whose running sum, with `before`, is over `target`; `by` times a value's weight is what it adds.
+template <class T>
+__device__ inline int pick_in_block(const RowChunks<T>& row, int block, float most, double scale, double by, double before, double target, int lane, float& logit) {
+    constexpr int VEC = Chunk<T>::VEC;
+    BlockChunks<T> held(row, block, lane);
+    double base = before;
+    int last = -1;
+    float last_logit = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < held.N; ++i) {
+        // chunk i in a loop that is not unrolled: by a chain of selections
+        Chunk<T> chunk = held.chunk[0];
+#pragma unroll
+        for (int j = 1; j < held.N; ++j)
+            if (i == j) chunk = held.chunk[j];
+        float x[VEC];
+        chunk.widen(x);
+        double w[VEC], mine = 0.0;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            w[e] = by * weight(x[e], most, scale);
+            mine += w[e];
+        }
+        const double upto = base + wave_scan(mine);
+        double at = __shfl_up(upto, 1);
+        if (lane == 0) at = base;
+        int found = -1, filled = -1;
+        float found_logit = 0.f, filled_logit = 0.f;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            at += w[e];
+            if (w[e] > 0.0) {
+                filled = e;
+                filled_logit = x[e];
+                if (found < 0 && at > target) {
+                    found = e;
+                    found_logit = x[e];
+                }
+            }
+        }
+        const int first = (block * (kBlock / VEC) + i * 64) * VEC - row.lead;
+        const uint64_t over = __ballot(found >= 0), some = __ballot(filled >= 0);
+        if (over) {
+            const int l = __ffsll((unsigned long long)over) - 1;
+            logit = __shfl(found_logit, l);
+            return first + l * VEC + __shfl(found, l);
+        }
+        if (some) {
+            const int l = 63 - __clzll((long long)some);
+            last = first + l * VEC + __shfl(filled, l);
+            last_logit = __shfl(filled_logit, l);
+        }
+        base = __shfl(upto, 63);
+    }
+    logit = last_logit;
+    return last;
+}
+
+// The token that a row's distribution has at the share u of its sum, or its most likely one; -1 without a distribution.
+template <class T>
+__device__ inline int draw(const VerifyIn& in, long long flat, const Norm& norm, bool greedy, double u, int lane, float& logit) {
+    if (!(norm.total > 0.0)) return -1;
+    const RowChunks<T> row(in.logits, flat, in.stride, in.vocab);
+    const BlockSum* blocks = in.blocks + flat * in.row_blocks;
+    const int count = (row.end + kBlock - 1) / kBlock;
+    if (greedy) {
+        int block = 0x7FFFFFFF;
+        for (int b = lane; b < count; b += 64)
+            if (blocks[b].most == norm.most) block = min(block, b);
+        for (int off = 32; off; off >>= 1) block = min(block, __shfl_xor(block, off));
+        BlockChunks<T> held(row, block, lane);
+        int token = 0x7FFFFFFF;
+#pragma unroll
+        for (int i = 0; i < held.N; ++i) {
+            float x[Chunk<T>::VEC];
+            held.chunk[i].widen(x);
+#pragma unroll
+            for (int e = 0; e < Chunk<T>::VEC; ++e)
+                if (x[e] == norm.most) token = min(token, (block * (kBlock / Chunk<T>::VEC) + i * 64 + lane) * Chunk<T>::VEC + e - row.lead);
+        }
+        for (int off = 32; off; off >>= 1) token = min(token, __shfl_xor(token, off));
+        logit = norm.most;
+        return token;
+    }
+    double before, all;
+    const auto of = [&](int b) { return blocks[b].most > -INFINITY ? blocks[b].sum * weight(blocks[b].most, norm.most, in.scale) : 0.0; };
+    const int block = pick_block(count, u, lane, before, of, all);
+    if (block < 0) return -1;
+    return pick_in_block<T>(row, block, blocks[block].most, in.scale, weight(blocks[block].most, norm.most, in.scale), before, u * all, lane, logit);
+}
+
+__device__ inline float log_probability(float logit, const Norm& norm, double scale) {
+    return (float)(((double)logit - (double)norm.most) * scale * 0.6931471805599453 - log(norm.total));
+}
+// of a row from which no token comes
+__device__ inline float no_probability(const Norm& norm) { return norm.total == 0.0 ? -INFINITY : NAN; }
+
+template <class T>
+__device__ inline int row_block_count(const VerifyIn& in, const void* data, long long r, long long stride) {
+    return (RowChunks<T>(data, r, stride, in.vocab).end + kBlock - 1) / kBlock;
+}
+
+constexpr int kWalkThreads = 1024;
+
+// Drafts that were not drawn: a workgroup a sequence, whose waves draw the tokens of all rows; then the way through the tree, a row a lane.
+template <class T>
+__global__ __launch_bounds__(kWalkThreads) void verify_tree_kernel(VerifyIn in) {
+    __shared__ int said[kMostDraft];
+    __shared__ float chances[kMostDraft];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = in.m;
+    const long long s = blockIdx.x;
+    const int count = in.count(s);
+    for (int i = wave; i < count; i += kWalkThreads / 64) {
+        const long long flat = s * m + i;
+        const Norm norm = row_norm(in.blocks + flat * in.row_blocks, row_block_count<T>(in, in.logits, flat, in.stride), in.scale, lane);
+        float logit = 0.f;
+        const int token = draw<T>(in, flat, norm, !in.uniforms, in.uniforms ? unit(in.uniforms[flat]) : 0.0, lane, logit);
+        if (lane == 0) {
+            said[i] = token;
+            chances[i] = token < 0 ? no_probability(norm) : log_probability(logit, norm, in.scale);
+        }
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    int up = -1, token = -1;
+    if (lane < count) {
+        up = in.parents ? in.parents[s * m + lane] : lane - 1;
+        if (up >= lane) up = -1;
+        token = in.tokens[s * m + lane];
+    }
+    int kept = 0, at = 0, following = -1;
+    int my_row = -1;                                  // of the path, at place `lane`
+    while (kept < count) {                            // a child comes behind its parent
+        if (lane == kept) my_row = at;
+        ++kept;
+        following = said[at];
+        const uint64_t children = __ballot(lane > 0 && lane < count && up == at && token == following && following >= 0);
+        if (!children) break;
+        at = __ffsll((unsigned long long)children) - 1;
+    }
+    if (lane < m) {
+        in.path[s * m + lane] = my_row;
+        in.logprobs[s * m + lane] = my_row >= 0 ? chances[my_row] : -INFINITY;
+    }
+    if (lane == 0) {
+        in.kept[s] = kept;
+        in.next[s] = following;
+    }
+}
+
+// A student's chain: which rows are kept, and the row where it ends.  A workgroup a sequence, a wave a row.
+template <class T>
+__global__ __launch_bounds__(kWalkThreads) void verify_chain_kernel(VerifyIn in) {
+    __shared__ Norm norms[kMostDraft], draft_norms[kMostDraft];
+    __shared__ int passes[kMostDraft];                // whether the row behind this one is kept
+    __shared__ float chances[kMostDraft];             // log p of the drafted token
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = in.m;
+    const long long s = blockIdx.x;
+    const int count = in.count(s);
+    for (int i = wave; i < count; i += kWalkThreads / 64) {
+        const long long flat = s * m + i;
+        const Norm norm = row_norm(in.blocks + flat * in.row_blocks, row_block_count<T>(in, in.logits, flat, in.stride), in.scale, lane);
+        Norm draft{-INFINITY, 0.0};
+        bool pass = false;
+        float chance = -INFINITY;
+        if (i + 1 < count) {
+            const long long r = s * (m - 1) + i;
+            draft = row_norm(in.blocks + (in.n * m + r) * in.row_blocks, row_block_count<T>(in, in.drafts, r, in.draft_stride), in.scale, lane);
+            if (!(draft.total > 0.0)) draft.total = 0.0;
+            const int token = in.tokens[flat + 1];
+            if (norm.total > 0.0 && token >= 0 && token < in.vocab) {
+                const float x = (float)((const T*)in.logits)[flat * in.stride + token];
+                const double p = weight(x, norm.most, in.scale) / norm.total;
+                double q = 0.0;
+                if (draft.total > 0.0) q = weight((float)((const T*)in.drafts)[r * in.draft_stride + token], draft.most, in.scale) / draft.total;
+                pass = unit(in.accept[flat + 1]) * q < p;
+                chance = log_probability(x, norm, in.scale);
+            }
+        }
+        if (lane == 0) {
+            norms[i] = norm;
+            draft_norms[i] = draft;
+            passes[i] = pass;
+            chances[i] = chance;
+        }
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    const uint64_t stops = __ballot(lane >= count || !passes[min(lane, max(count - 1, 0))]);
+    const int stop = count ? min(__ffsll((unsigned long long)stops) - 1, count - 1) : -1;
+    if (lane < m) {
+        in.path[s * m + lane] = lane <= stop ? lane : -1;
+        if (lane != stop) in.logprobs[s * m + lane] = lane < stop ? chances[lane] : -INFINITY;
+    }
+    if (lane == 0) {
+        in.kept[s] = stop + 1;
+        Stop to{};
+        to.row = stop;
+        if (stop >= 0) {
+            to.most = norms[stop].most;
+            to.total = norms[stop].total;
+            to.drafted = stop + 1 < count && draft_norms[stop].total > 0.0;
+            to.draft_most = draft_norms[stop].most;
+            to.draft_total = draft_norms[stop].total;
+        }
+        in.stops[s] = to;
+    }
+}
+
+// max(p - q, 0) of a token of the row where a chain ends
+template <class T>
+__device__ inline double left_of(const Stop& stop, const T* logits, const T* drafts, int token, double scale) {
+    const double p = weight((float)logits[token], stop.most, scale) / stop.total;
+    const double q = weight((float)drafts[token], stop.draft_most, scale) / stop.draft_total;
+    return fmax(p - q, 0.0);
+}
+template <class T>
+__device__ inline const T* draft_row(const VerifyIn& in, long long s, int i) {
+    return (const T*)in.drafts + (s * (in.m - 1) + i) * in.draft_stride;
+}
+
+// The sums of max(p - q, 0) over blocks of the rows where chains end, a wave a block.
+template <class T>
+__global__ __launch_bounds__(kSumThreads) void left_sums_kernel(VerifyIn in) {
+    const int lane = threadIdx.x & 63;
+    const long long item = (long long)blockIdx.x * (kSumThreads / 64) + (threadIdx.x >> 6);
+    const long long s = item / in.left_blocks;
+    const int block = (int)(item % in.left_blocks);
+    if (s >= in.n) return;
+    const Stop stop = in.stops[s];
+    if (stop.row < 0 || !stop.drafted || !(stop.total > 0.0)) return;
+    const T* x = (const T*)in.logits + (s * in.m + stop.row) * in.stride;
+    const T* y = draft_row<T>(in, s, stop.row);
+    double sum = 0.0;
+    for (int i = 0; i < kLaneValues; ++i) {
+        const int token = block * kBlock + i * 64 + lane;
+        if (token < in.vocab) sum += left_of(stop, x, y, token, in.scale);
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) in.left[s * in.left_blocks + block] = sum;
+}
+
+// The next token of a chain, a wave a sequence.
+template <class T>
+__global__ __launch_bounds__(64) void draw_left_kernel(VerifyIn in) {
+    const int lane = threadIdx.x;
+    const long long s = blockIdx.x;
+    const Stop stop = in.stops[s];
+    if (stop.row < 0) {
+        if (lane == 0) in.next[s] = -1;
+        return;
+    }
+    const long long flat = s * in.m + stop.row;
+    const Norm norm{stop.most, stop.total};
+    const double u = unit(in.uniforms[flat]);
+    int token = -1;
+    float logit = 0.f;
+    if (stop.drafted && norm.total > 0.0) {
+        const double* left = in.left + s * in.left_blocks;
+        double before, all;
+        const int block = pick_block(in.left_blocks, u, lane, before, [&](int b) { return left[b]; }, all);
+        if (block >= 0) {
+            const T* x = (const T*)in.logits + flat * in.stride;
+            const T* y = draft_row<T>(in, s, stop.row);
+            double base = before;
+            int last = -1;
+            for (int i = 0; i < kLaneValues && token < 0; ++i) {
+                const int v = block * kBlock + i * 64 + lane;
+                const double mine = v < in.vocab ? left_of(stop, x, y, v, in.scale) : 0.0;
+                const double upto = base + wave_scan(mine);
+                const uint64_t over = __ballot(mine > 0.0 && upto > u * all), some = __ballot(mine > 0.0);
+                if (over) token = block * kBlock + i * 64 + __ffsll((unsigned long long)over) - 1;
+                if (some) last = block * kBlock + i * 64 + 63 - __clzll((long long)some);
+                base = __shfl(upto, 63);
+            }
+            if (token < 0) token = last;
+            if (token >= 0) logit = (float)x[token];
+        }
+    }
+    if (token < 0) token = draw<T>(in, flat, norm, false, u, lane, logit);
+    if (lane == 0) {
+        in.next[s] = token;
+        in.logprobs[flat] = token < 0 ? no_probability(norm) : log_probability(logit, norm, in.scale);
+    }
+}
+
+// ---- launches
+
+int row_blocks(int32_t vocab) { return (int)(((int64_t)vocab + 7 + kBlock - 1) / kBlock); }      // at the worst alignment
+int left_blocks(int32_t vocab) { return (int)(((int64_t)vocab + kBlock - 1) / kBlock); }
+
+struct VerifySpace {
+    size_t blocks, left, stops;
+    size_t bytes() const { return blocks + left + stops; }
+};
+VerifySpace verify_space(int64_t n, int32_t m, int32_t vocab, bool drafts) {
+    VerifySpace v{};
+    v.blocks = align_up((size_t)(n * m + (drafts ? n * (m - 1) : 0)) * row_blocks(vocab) * sizeof(BlockSum));
+    if (drafts) {
+        v.left = align_up((size_t)n * left_blocks(vocab) * sizeof(double));
+        v.stops = align_up((size_t)n * sizeof(Stop));
+    }
+    return v;
+}
+
+constexpr int64_t kMostRows = 1 << 21;
+constexpr int64_t kMostBlocks = (int64_t)1 << 25;            // a wave each: a launch has fewer than 2^32 threads
+
+bool verify_shape(int64_t n, int32_t m, int32_t vocab) {
+    return n >= 1 && m >= 1 && m <= kMostDraft && vocab >= 1 && vocab <= (1 << 30) && n <= kMostRows && 2 * n * m <= kMostRows && 2 * n * m * row_blocks(vocab) <= kMostBlocks;
+}
+
+template <class T>
+int launch_verify(const VerifyIn& in, hipStream_t stream) {
+    const int64_t rows = in.n * in.m + (in.drafts ? in.n * (in.m - 1) : 0);
+    constexpr int kWaves = kSumThreads / 64;
+    hipLaunchKernelGGL((block_sums_kernel<T>), dim3((unsigned)((rows * in.row_blocks + kWaves - 1) / kWaves)), dim3(kSumThreads), 0, stream, in);
+    HIP_TRY(hipGetLastError());
+    if (!in.drafts) {
+        hipLaunchKernelGGL((verify_tree_kernel<T>), dim3((unsigned)in.n), dim3(kWalkThreads), 0, stream, in);
+        HIP_TRY(hipGetLastError());
+        return IVFPQ_OK;
+    }
+    hipLaunchKernelGGL((verify_chain_kernel<T>), dim3((unsigned)in.n), dim3(kWalkThreads), 0, stream, in);
+    HIP_TRY(hipGetLastError());
+    hipLaunchKernelGGL((left_sums_kernel<T>), dim3((unsigned)((in.n * in.left_blocks + kWaves - 1) / kWaves)), dim3(kSumThreads), 0, stream, in);
+    HIP_TRY(hipGetLastError());
+    hipLaunchKernelGGL((draw_left_kernel<T>), dim3((unsigned)in.n), dim3(64), 0, stream, in);
+    HIP_TRY(hipGetLastError());
+    return IVFPQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ivfpq_verify_drafts_workspace_bytes(int64_t n, int32_t m, int32_t vocab, int32_t with_drafts) {
+    return verify_shape(n, m, vocab) ? verify_space(n, m, vocab, with_drafts != 0).bytes() : 0;
+}
+
+int ivfpq_verify_drafts(const void* d_logits, int32_t dtype, int64_t n, int32_t m, int32_t vocab, int64_t row_stride, const int32_t* d_tokens,
+                        const int32_t* d_parents, const int32_t* d_counts, const float* d_uniforms, double temperature, const void* d_draft_logits,
+                        int64_t draft_stride, const float* d_accept, int32_t* d_path, int32_t* d_kept, int32_t* d_next, float* d_logprobs,
+                        void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    return guarded("ivfpq_verify_drafts", [&] {
+        const char* what = "ivfpq_verify_drafts";
+        if (!known_dtype(dtype)) return fail(IVFPQ_EINVAL, "%s: unknown dtype %d", what, dtype);
+        if (n < 0 || m < 1 || vocab < 1) return fail(IVFPQ_EINVAL, "%s: bad shape (n=%lld m=%d vocab=%d)", what, (long long)n, m, vocab);
+        if (m > kMostDraft) return fail(IVFPQ_EUNSUPPORTED, "%s: m=%d (limit %d rows)", what, m, kMostDraft);
+        if (vocab > (1 << 30)) return fail(IVFPQ_EUNSUPPORTED, "%s: vocab=%d (limit 2^30)", what, vocab);
+        if (!(temperature >= 1e-6 && temperature <= 1e6)) return fail(IVFPQ_EINVAL, "%s: temperature outside [1e-6, 1e6]", what);
+        if (d_draft_logits && d_parents) return fail(IVFPQ_EINVAL, "%s: drafts that were drawn are a chain, without parents", what);
+        if (n == 0) return (int)IVFPQ_OK;
+        if (!verify_shape(n, m, vocab)) return fail(IVFPQ_EUNSUPPORTED, "%s: n=%lld m=%d vocab=%d: over the limits (2^20 rows, 2^24 blocks of 2048 logits)", what, (long long)n, m, vocab);
+        if (!d_logits || !d_tokens || !d_path || !d_kept || !d_next || !d_logprobs) return fail(IVFPQ_EINVAL, "%s: null pointer", what);
+        if (d_draft_logits && (!d_uniforms || !d_accept)) return fail(IVFPQ_EINVAL, "%s: drafts that were drawn need both random numbers", what);
+        if (n * m > 1 && row_stride < vocab) return fail(IVFPQ_EINVAL, "%s: row stride %lld below vocab=%d", what, (long long)row_stride, vocab);
+        if (d_draft_logits && n * (m - 1) > 1 && draft_stride < vocab) return fail(IVFPQ_EINVAL, "%s: draft stride %lld below vocab=%d", what, (long long)draft_stride, vocab);
+        if ((uintptr_t)d_logits % value_bytes(dtype) || (uintptr_t)d_draft_logits % value_bytes(dtype)) return fail(IVFPQ_EINVAL, "%s: logits are not aligned to their type", what);
+        const bool drafts = d_draft_logits && m > 1;       // one row drafts nothing
+        const VerifySpace space = verify_space(n, m, vocab, drafts);
+        if (!d_workspace) return fail(IVFPQ_EINVAL, "%s: null workspace", what);
+        if ((uintptr_t)d_workspace % kAlign) return fail(IVFPQ_EINVAL, "%s: workspace not aligned to %zu bytes", what, kAlign);
+        if (workspace_bytes < space.bytes()) return fail(IVFPQ_ENOSPACE, "%s: workspace %zu bytes, need %zu", what, workspace_bytes, space.bytes());
+        char* ws = (char*)d_workspace;
+        const VerifyIn in{d_logits, drafts ? d_draft_logits : nullptr, row_stride, draft_stride, d_tokens, d_parents, d_counts, d_uniforms, d_accept,
+                          (BlockSum*)ws, (double*)(ws + space.blocks), (Stop*)(ws + space.blocks + space.left), d_path, d_kept, d_next, d_logprobs, n, m, vocab,
+                          row_blocks(vocab), left_blocks(vocab), 1.4426950408889634 / temperature};
+        return with_value_type(dtype, [&](auto t) { return launch_verify<decltype(t)>(in, (hipStream_t)hip_stream); });
+    });
+}
+
+}  // extern "C"
