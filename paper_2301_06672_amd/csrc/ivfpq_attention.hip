@@ -51,7 +51,8 @@ struct AttentionIn {
     const int* parents;               // [n][m] or null
     long long q_stride, out_stride, n;
     int heads, blocks, splits;
-    float scale;                      // with log2(e)
+    float scale;                      // its size, with log2(e): not 0, so that -inf stays what it is
+    bool negative;
     Pages at;
 };
 
@@ -60,127 +61,90 @@ constexpr int kAttentionThreads = 256, kTile = 32;
 // 65,504), and those under 2^-24 of the largest, which fp16 would cut off, are kept down to 2^-30.
 constexpr float kBelow = 6.f, kAhead = 14.f;
 
-// T: type of the cache.  KC: 32 components of a head each (d <= 32 KC; EXACT: equal).  NQ: tiles of 16 columns a wave.  APART: a wave has columns of its
-// own and goes over all places of the workgroup; otherwise the four waves share their columns, take every fourth tile, and add up at the end.
-template <class T, int KC, int NQ, bool APART, bool EXACT>
-__global__ __launch_bounds__(kAttentionThreads) void attention_kernel(AttentionIn in) {
-    constexpr int VT = KC * 2;                       // tiles of 16 components
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 15, group = lane >> 4;
-    const int d = EXACT ? KC * 32 : in.at.d;
-    const int shift = in.at.shift, in_page = in.at.page() - 1;
+// What sums about one reference are multiplied by for a larger one.  Not 0: an infinity among them stays one, and what is under 2^-126 of others is lost
+// in them anyway.
+__device__ inline float shrink_by(float from, float to) { return from == to || from == -INFINITY ? 1.f : fmaxf(exp2_fast(from - to), 0x1p-126f); }
 
-    // blocks of columns that read the same places are 8 workgroups apart: on one XCD, whose L2 they share
-    const unsigned order = blockIdx.x, turn = order / 8;
-    const int block = (int)(turn % in.blocks);
-    const long long pass = (long long)(turn / in.blocks) * 8 + order % 8;      // (split, head, sequence)
-    if (pass >= in.n * in.at.kv_heads * in.splits) return;
-    const long long s = pass % in.n;
-    const int head = (int)(pass / in.n % in.at.kv_heads), split = (int)(pass / in.n / in.at.kv_heads);
-    const int share = in.heads / in.at.kv_heads;     // heads that share keys
-    const int len = in.at.len(s), count = in.at.count(s), m = in.at.m;
-    const int first_col = (block * (APART ? 4 : 1) + (APART ? wave : 0)) * NQ * 16;
-    const int all_cols = m * share, used_cols = count * share;
-
-    // what each column sees of the rows: bits of a tree, or the rows up to its own
+// What a lane has to know of a column: its row and what that sees of the rows.
+__device__ inline uint64_t tree_line(const AttentionIn& in, long long s, int count, int lane) {
     uint64_t line = 0;
-    if (in.parents) {
-        int up = -1;
-        if (lane < count) {
-            up = in.parents[s * m + lane];
-            if (up < 0 || up >= lane) up = -1;
-            line = (uint64_t)1 << lane;
+    int up = -1;
+    if (lane < count) {
+        up = in.parents[s * in.at.m + lane];
+        if (up < 0 || up >= lane) up = -1;
+        line = (uint64_t)1 << lane;
+    }
+    for (int far = 1; far < 64; far *= 2) {          // a row has up to 63 ancestors
+        const uint64_t above = __shfl((unsigned long long)line, max(up, 0));
+        const int next = __shfl(up, max(up, 0));
+        if (up >= 0) {
+            line |= above;
+            up = next;
         }
-        for (int far = 1; far < 64; far *= 2) {      // a row has up to 63 ancestors
-            const uint64_t above = __shfl((unsigned long long)line, max(up, 0));
-            const int next = __shfl(up, max(up, 0));
-            if (up >= 0) {
-                line |= above;
-                up = next;
+    }
+    return line;
+}
+
+// The pages of a tile's two halves; -1: not there.  Such a half is read as page 0 (there is one: without pages there are no tiles), and the tile is gone
+// over with a mask.
+struct TilePages {
+    int first, second;
+    __device__ inline bool both() const { return first >= 0 && second >= 0; }
+};
+__device__ inline TilePages tile_pages(const Pages& at, const int* pages, int tile, int end) {
+    const long long place = (long long)tile * kTile, i0 = place >> at.shift, i1 = (place + 16) >> at.shift;
+    TilePages p{tile < end && i0 < at.most ? pages[i0] : -1, tile < end && i1 < at.most ? pages[i1] : -1};
+    if (p.first >= at.n_pages) p.first = -1;
+    if (p.second >= at.n_pages) p.second = -1;
+    return p;
+}
+
+// A wave's columns: NQ tiles of 16 with d <= 32 KC components (EXACT: equal), and what they have summed up.
+template <class T, int KC, int NQ, bool EXACT>
+struct Columns {
+    static constexpr int VT = KC * 2;                // tiles of 16 components
+    u32x4 q[NQ][KC];
+    f32x4 sums[NQ][VT];
+    float reference[NQ], total[NQ];
+    int row[NQ];                                     // -1: nothing to do in this column
+    uint64_t sees[NQ];                               // rows of a tree
+
+    __device__ inline void start(const AttentionIn& in, long long s, int head, int first_col, int count, uint64_t line, int d, int lane) {
+        const int share = in.heads / in.at.kv_heads, col = lane & 15, group = lane >> 4;
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) {
+            const int x = first_col + t * 16 + col;
+            row[t] = x < count * share ? x / share : -1;
+            sees[t] = __shfl((unsigned long long)line, max(row[t], 0) & 63);
+            const T* from = (const T*)in.q + (s * in.at.m + max(row[t], 0)) * in.q_stride + (long long)(head * share + x % share) * d + group * 8;
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                q[t][c] = row[t] >= 0 && (EXACT || c * 32 + group * 8 < d) ? *reinterpret_cast<const u32x4*>(from + c * 32) : u32x4{};
+                if (in.negative) q[t][c] ^= 0x80008000u;
+            }
+            reference[t] = -INFINITY;
+            total[t] = 0.f;
+#pragma unroll
+            for (int v = 0; v < VT; ++v) sums[t][v] = f32x4{};
+        }
+    }
+
+    // Many columns' queries and sums stay in the registers that matrix instructions take and give their operands in.  Left to itself the compiler
+    // moves all sums to others and back once a tile, since they are scaled there now and then.
+    __device__ inline void settle() {
+        if constexpr (NQ * KC >= 8) {
+#pragma unroll
+            for (int t = 0; t < NQ; ++t) {
+#pragma unroll
+                for (int c = 0; c < KC; ++c) asm volatile("" : "+a"(q[t][c]));
+#pragma unroll
+                for (int v = 0; v < VT; ++v) asm volatile("" : "+a"(sums[t][v]));
             }
         }
     }
-    u32x4 q[NQ][KC];
-    int row[NQ];
-    uint64_t sees[NQ];
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-        const int x = first_col + t * 16 + col;
-        row[t] = x < used_cols ? x / share : -1;     // -1: nothing to do in this column
-        sees[t] = __shfl((unsigned long long)line, max(row[t], 0) & 63);
-        const T* from = (const T*)in.q + (s * m + max(row[t], 0)) * in.q_stride + (long long)(head * share + x % share) * d + group * 8;
-#pragma unroll
-        for (int c = 0; c < KC; ++c) q[t][c] = row[t] >= 0 && (EXACT || c * 32 + group * 8 < d) ? *reinterpret_cast<const u32x4*>(from + c * 32) : u32x4{};
-    }
-    f32x4 sums[NQ][VT];
-    float reference[NQ], total[NQ];
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-        reference[t] = -INFINITY;
-        total[t] = 0.f;
-#pragma unroll
-        for (int v = 0; v < VT; ++v) sums[t][v] = f32x4{};
-    }
 
-    // tiles of the workgroup: of the places up to the last that one of its columns sees
-    const int block_cols = NQ * 16 * (APART ? 4 : 1);
-    const int last_col = min((block + 1) * block_cols, used_cols) - 1;
-    const bool nothing = block * block_cols >= used_cols;
-    const long long places = nothing ? 0 : in.parents ? (long long)len + count : (long long)len + last_col / share + 1;
-    const int tiles = (int)min((places + kTile - 1) / kTile, (((long long)in.at.most << shift) + kTile - 1) / kTile);
-    constexpr int STEP = APART ? 1 : 4;
-    int each = (tiles + in.splits - 1) / in.splits;
-    each = (each + STEP - 1) / STEP * STEP;
-    const int first = (int)min((long long)split * each, (long long)tiles), end = min(first + each, tiles);
-    const int* pages = in.at.pages + s * in.at.stride;
-
-    const long long page_values = in.at.page_values();
-    const int key_in_tile = (col >> 2) * 8 + (col & 3);             // and 4 more in the second half of S
-    const bool second_k = col >> 3, second_v = group >> 1;          // in the tile's second 16 places
-    const int k_lane = (key_in_tile & 15) * d + group * 8, v_lane = (group & 1) * 8 * d + col * 8;
-    const T* const k_head = (const T*)in.k_cache + ((long long)head << shift) * d;
-    const T* const v_head = (const T*)in.v_cache + ((long long)head << shift) * d;
-
-    // The pages of a tile's two halves; one that is not there is read as page 0 (there is one: without pages there are no tiles), and the tile is
-    // gone over with a mask.
-    const auto find = [&](int tile, int& p0, int& p1) {
-        const long long at = (long long)tile * kTile, i0 = at >> shift, i1 = (at + 16) >> shift;
-        p0 = tile < end && i0 < in.at.most ? pages[i0] : -1;
-        p1 = tile < end && i1 < in.at.most ? pages[i1] : -1;
-        if (p0 >= in.at.n_pages) p0 = -1;
-        if (p1 >= in.at.n_pages) p1 = -1;
-    };
-    u32x4 keys[2][KC], values[VT];
-    const auto load_keys = [&](int tile, int p0, int p1) {
-        const int off0 = (tile * kTile) & in_page, off1 = (tile * kTile + 16) & in_page;
-        const T* from = k_head + (second_k ? max(p1, 0) * page_values + off1 * d : max(p0, 0) * page_values + off0 * d) + k_lane;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int c = 0; c < KC; ++c) keys[t][c] = EXACT || c * 32 + group * 8 < d ? *reinterpret_cast<const u32x4*>(from + t * 4 * d + c * 32) : u32x4{};
-    };
-    const auto load_values = [&](int tile, int p0, int p1) {
-        const int off0 = (tile * kTile) & in_page, off1 = (tile * kTile + 16) & in_page;
-        const T* from = v_head + (second_v ? max(p1, 0) * page_values + off1 * d : max(p0, 0) * page_values + off0 * d) + v_lane;
-#pragma unroll
-        for (int v = 0; v < VT; ++v) values[v] = EXACT || v * 16 + col < d ? *reinterpret_cast<const u32x4*>(from + v * 128) : u32x4{};
-    };
-
-    int tile = first + (APART ? 0 : wave);
-    int page0 = -1, page1 = -1, next0 = -1, next1 = -1;
-    find(tile, page0, page1);
-    find(tile + STEP, next0, next1);
-    if (tile < end) {
-        load_keys(tile, page0, page1);
-        load_values(tile, page0, page1);
-    }
-    // One tile; the next one's keys are loaded as soon as this one's are used, and its values likewise.
-    const auto go = [&](auto masked) {
-        constexpr bool MASKED = decltype(masked)::value;
-        int after0, after1;
-        find(tile + 2 * STEP, after0, after1);
-        const bool more = tile + STEP < end;
-        f32x4 score[NQ][2];
+    // S of a tile: the product of its keys, whose rows are dealt as key_place says, and the queries
+    __device__ inline void scores(const u32x4 (&keys)[2][KC], f32x4 (&score)[NQ][2]) const {
 #pragma unroll
         for (int t = 0; t < NQ; ++t)
 #pragma unroll
@@ -190,200 +154,400 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_kernel(AttentionI
                 for (int c = 0; c < KC; ++c) acc = multiply<T>(keys[h][c], q[t][c], acc);
                 score[t][h] = acc;
             }
-        if (more) load_keys(tile + STEP, next0, next1);
+    }
 
-        // weights in the order of the places 8 group + j; one that a column does not see is 0
-        const int first_place = tile * kTile + group * 8;
-        const bool there = second_v ? page1 >= 0 : page0 >= 0;       // the page of this lane's places
-        u32x4 weights[NQ];
-        unsigned hidden[NQ];
+    // Bits of 8 places, from `first_place` on, that column t sees; there: their page is.
+    __device__ inline unsigned seen(const AttentionIn& in, int t, int first_place, int len, bool there) const {
+        const int behind = first_place - len;        // row that the first of them is the place of
+        const unsigned cached = behind >= 0 ? 0u : (1u << min(-behind, 8)) - 1;
+        unsigned rows;
+        if (in.parents) rows = behind >= 64 || behind <= -8 ? 0u : (unsigned)(behind >= 0 ? sees[t] >> behind : sees[t] << -behind);
+        else rows = (1u << min(max(row[t] - behind + 1, 0), 8)) - 1;
+        return there && row[t] >= 0 ? (cached | rows) & 0xFF : 0u;
+    }
+    // What columns do not see of the lane's places becomes -inf.
+    __device__ inline void mask(const AttentionIn& in, f32x4 (&score)[NQ][2], int first_place, int len, bool there) const {
 #pragma unroll
         for (int t = 0; t < NQ; ++t) {
-            float w[8];
-            hidden[t] = 0;
+            const unsigned bits = seen(in, t, first_place, len, there);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = score[t][j >> 2][j & 3] * in.scale;
-            if constexpr (MASKED) {
+            for (int j = 0; j < 8; ++j) score[t][j >> 2][j & 3] = bits >> j & 1 ? score[t][j >> 2][j & 3] : -INFINITY;
+        }
+    }
+    // 0 times infinity is no number, so in a tile that not every column sees whole such values must not meet weights of 0: those of places without a row
+    // (bits of `holds` unset, by halves of words) go, and infinities and NaNs of rows become 0.  -> whether there were any.
+    __device__ inline bool tame(u32x4 (&values)[VT], const u32x4& holds) const {
+        constexpr uint32_t kOnes = std::is_same<T, half_t>::value ? 0x7C00u : 0x7F80u;
+        bool odd = false;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int behind = first_place + j - len;        // row whose place it is
-                    const bool drafted = in.parents ? behind < 64 && (sees[t] >> (behind & 63) & 1) : behind <= row[t];
-                    if (!(there && row[t] >= 0 && (behind < 0 || drafted))) {
-                        w[j] = -INFINITY;
-                        hidden[t] |= 1u << j;
-                    }
-                }
+        for (int v = 0; v < VT; ++v)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t x = values[v][i] & holds[i];
+                const bool low = (x & kOnes) == kOnes, high = (x & kOnes << 16) == kOnes << 16;
+                x = low ? x & 0xFFFF0000u : x;
+                x = high ? x & 0xFFFFu : x;
+                odd |= low | high;
+                values[v][i] = x;
             }
-            float most = max3(max3(w[0], w[1], w[2]), max3(w[3], w[4], w[5]), fmaxf(w[6], w[7]));
-            if (__any(most > reference[t] + kAhead)) {
-                most = fmaxf(most, __shfl_xor(most, 16));
-                most = fmaxf(most, __shfl_xor(most, 32));
-                const float now = fmaxf(reference[t], most - kBelow);
-                const float shrink = now == reference[t] ? 1.f : exp2_fast(reference[t] - now);
+        return odd;
+    }
+    // What the infinities and NaNs that tame() took make of the sums: themselves in every column that sees them, or NaN if its weight is 0.
+    // Over the tiles [first, end) that are `step` apart; seldom called, so slow and small.
+    __device__ inline void add_odd(const AttentionIn& in, long long s, int head, int first_col, int first, int end, int step, int len, int d, int lane) {
+        const int col = lane & 15, group = lane >> 4, share = in.heads / in.at.kv_heads;
+#pragma unroll 1
+        for (int place = first * kTile; place < end * kTile; place = place % kTile == kTile - 1 ? place + 1 + (step - 1) * kTile : place + 1) {
+            const int page = in.at.page_of(s, place), off = place & (in.at.page() - 1);
+            if (page < 0) continue;
+            const long long base = page * in.at.page_values() + ((long long)head << in.at.shift) * d;
+            const T* v_at = (const T*)in.v_cache + base + (off >> 3) * 8 * d + (off & 7);
+            const T* k_at = (const T*)in.k_cache + base + off * d;
+            bool any = false;
+#pragma unroll 1
+            for (int c = lane; c < d; c += 64) any |= !(fabsf((float)v_at[c * 8]) < INFINITY);
+            if (!__any(any)) continue;
+#pragma unroll
+            for (int t = 0; t < NQ; ++t) {
+                if (!(seen(in, t, place, len, true) & 1)) continue;
+                const T* x = (const T*)in.q + (s * in.at.m + row[t]) * in.q_stride + (long long)(head * share + (first_col + t * 16 + col) % share) * d;
+                float score = 0.f;
+#pragma unroll 1
+                for (int c = 0; c < d; ++c) score = __builtin_fmaf((float)x[c], (float)k_at[c], score);
+                const float w = score == (in.negative ? INFINITY : -INFINITY) ? 0.f : 1.f;
+#pragma unroll
+                for (int v = 0; v < VT; ++v)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int c = v * 16 + group * 4 + i;
+                        if (!EXACT && c >= d) continue;
+                        const float value = (float)v_at[c * 8];
+                        sums[t][v][i] += fabsf(value) < INFINITY ? 0.f : w * value;
+                    }
+            }
+        }
+    }
+
+    // Scores, still without the scale, to weights, as the second product's operand (the places 8 group + j are the lane's in both), and the
+    // second product.
+    __device__ inline void weigh_and_add(f32x4 (&score)[NQ][2], float scale, const u32x4 (&values)[VT]) {
+        bool ahead = false;
+        float most[NQ];
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) {
+            most[t] = scale * max3(max3(score[t][0][0], score[t][0][1], score[t][0][2]), max3(score[t][0][3], score[t][1][0], score[t][1][1]), fmaxf(score[t][1][2], score[t][1][3]));
+            ahead |= most[t] > reference[t] + kAhead;
+        }
+        if (__any(ahead)) {
+#pragma unroll
+            for (int t = 0; t < NQ; ++t) {
+                most[t] = fmaxf(most[t], __shfl_xor(most[t], 16));
+                most[t] = fmaxf(most[t], __shfl_xor(most[t], 32));
+                const float now = fmaxf(reference[t], most[t] - kBelow);
+                const float shrink = shrink_by(reference[t], now);
                 reference[t] = now;
                 total[t] *= shrink;
 #pragma unroll
                 for (int v = 0; v < VT; ++v) sums[t][v] *= shrink;
             }
-            const float r = reference[t] == -INFINITY ? 0.f : reference[t];      // nothing seen so far
-#pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = exp2_fast(w[j] - r);
-            total[t] += tree_sum<8>(w);
-            weights[t] = narrow8<T>(w);
         }
+        settle();
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) {
+            const float r = reference[t] == -INFINITY ? 0.f : reference[t];      // nothing seen so far
+            float w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = exp2_fast(__builtin_fmaf(score[t][j >> 2][j & 3], scale, -r));
+            total[t] += tree_sum<8>(w);
+            const u32x4 weights = narrow8<T>(w);
+#pragma unroll
+            for (int v = 0; v < VT; ++v) sums[t][v] = multiply<T>(values[v], weights, sums[t][v]);
+        }
+    }
 
-        if constexpr (!MASKED) {
+    // a column's lanes hold sums of all its places, but each the total of its own 8 of every 32
+    __device__ inline void finish() {
 #pragma unroll
-            for (int t = 0; t < NQ; ++t)
+        for (int t = 0; t < NQ; ++t) {
+            total[t] += __shfl_xor(total[t], 16);
+            total[t] += __shfl_xor(total[t], 32);
+            if (row[t] < 0) {                        // went along with the others over the tiles without a mask
+                total[t] = 0.f;
+                reference[t] = -INFINITY;
 #pragma unroll
-                for (int v = 0; v < VT; ++v) sums[t][v] = multiply<T>(values[v], weights[t], sums[t][v]);
-        } else {
-            // 0 times infinity is no number, so values that not every column sees must not meet weights of 0: those of places without a row go, and
-            // infinities and NaNs of rows are added to the columns that see them, place by place
-            constexpr uint32_t kOnes = std::is_same<T, half_t>::value ? 0x7C00u : 0x7F80u;
-            const auto wild = [&](uint32_t x) {       // the halves of a word that are infinities or NaNs
-                return ((x & kOnes) == kOnes ? 0xFFFFu : 0u) | ((x & kOnes << 16) == kOnes << 16 ? 0xFFFF0000u : 0u);
-            };
-            uint32_t odd[4] = {0, 0, 0, 0};
+                for (int v = 0; v < VT; ++v) sums[t][v] = f32x4{};
+            }
+        }
+    }
+
+    __device__ inline void write(const AttentionIn& in, long long s, int head, int split, int first_col, int d, int lane) const {
+        const int share = in.heads / in.at.kv_heads, col = lane & 15, group = lane >> 4;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t holds = (there && first_place + 2 * i < places ? 0xFFFFu : 0u) | (there && first_place + 2 * i + 1 < places ? 0xFFFF0000u : 0u);
+        for (int t = 0; t < NQ; ++t) {
+            const int x = first_col + t * 16 + col;
+            if (x >= in.at.m * share) continue;
+            const int h = head * share + x % share;
+            const long long flat = s * in.at.m + x / share;
+            if (in.splits > 1) {
+                const long long at = (flat * in.heads + h) * in.splits + split;
+                if (group == 0) in.norms[at] = make_float2(reference[t], total[t]);
 #pragma unroll
                 for (int v = 0; v < VT; ++v) {
-                    values[v][i] &= holds;
-                    odd[i] |= wild(values[v][i]);
+                    const int c = v * 16 + group * 4;
+                    if (EXACT || c < d) *reinterpret_cast<f32x4*>(in.sums + at * d + c) = sums[t][v];
                 }
-            }
-            if (__any((odd[0] | odd[1] | odd[2] | odd[3]) != 0)) {
-#pragma unroll 1
-                for (int place = 0; place < kTile; ++place) {
-                    const int g = place >> 3, j = place & 7;
-                    const uint32_t field = 0xFFFFu << (j & 1) * 16, mine = j < 2 ? odd[0] : j < 4 ? odd[1] : j < 6 ? odd[2] : odd[3];
-                    if (!__any(group == g && (mine & field))) continue;
-                    bool seen[NQ];
-#pragma unroll
-                    for (int t = 0; t < NQ; ++t) seen[t] = row[t] >= 0 && !(__shfl(hidden[t], g * 16 + col) >> j & 1);
-#pragma unroll
-                    for (int v = 0; v < VT; ++v) {
-                        u32x4 one;                   // this place's values, where they are odd
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) one[i] = group == g && i == j >> 1 ? values[v][i] & field & wild(values[v][i]) : 0u;
-#pragma unroll
-                        for (int t = 0; t < NQ; ++t) {
-                            const f32x4 with = multiply<T>(one, weights[t], sums[t][v]);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) sums[t][v][i] = seen[t] ? with[i] : sums[t][v][i];
-                        }
-                    }
-                }
+            } else {
+                const float by = total[t] == 0.f ? 0.f : 1.f / total[t];
+                if (in.lse && group == 0) in.lse[flat * in.heads + h] = total[t] == 0.f ? -INFINITY : (reference[t] + __log2f(total[t])) * kLn2;
+                T* to = (T*)in.out + flat * in.out_stride + (long long)h * d + group * 4;
 #pragma unroll
                 for (int v = 0; v < VT; ++v)
+                    if (EXACT || v * 16 + group * 4 < d) {
+                        typedef T v4 __attribute__((ext_vector_type(4)));
+                        v4 y;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) values[v][i] &= ~wild(values[v][i]);
+                        for (int i = 0; i < 4; ++i) y[i] = (T)(sums[t][v][i] * by);
+                        *reinterpret_cast<v4*>(to + v * 16) = y;
+                    }
             }
-#pragma unroll
-            for (int t = 0; t < NQ; ++t)
-#pragma unroll
-                for (int v = 0; v < VT; ++v) sums[t][v] = multiply<T>(values[v], weights[t], sums[t][v]);
         }
-        if (more) load_values(tile + STEP, next0, next1);
-        page0 = next0, page1 = next1;
-        next0 = after0, next1 = after1;
+    }
+};
+
+// What a workgroup does: a block of columns of a head of a sequence over a part of the tiles of places.
+struct Piece {
+    long long s;
+    int head, split, block, len, count, first, end;
+    long long places;                                // up to the last that one of the columns sees
+    bool nothing;                                    // no such piece
+};
+// cols: of a block; STEP: tiles that a part's number of tiles is a multiple of.
+__device__ inline Piece piece_of(const AttentionIn& in, int cols, int step) {
+    // blocks of columns that read the same places are 8 workgroups apart: on one XCD, whose L2 they share
+    const unsigned order = blockIdx.x, turn = order / 8;
+    Piece p{};
+    p.block = (int)(turn % in.blocks);
+    const unsigned pass = turn / in.blocks * 8 + order % 8, n = (unsigned)in.n;      // (split, head, sequence); under 2^23 workgroups
+    p.nothing = pass >= n * (unsigned)(in.at.kv_heads * in.splits);
+    if (p.nothing) return p;
+    p.s = pass % n;
+    p.head = (int)(pass / n % in.at.kv_heads);
+    p.split = (int)(pass / n / in.at.kv_heads);
+    p.len = in.at.len(p.s);
+    p.count = in.at.count(p.s);
+    const int share = in.heads / in.at.kv_heads, used = p.count * share, last_col = min((p.block + 1) * cols, used) - 1;
+    p.places = p.block * cols >= used ? 0 : in.parents ? (long long)p.len + p.count : (long long)p.len + last_col / share + 1;
+    const int tiles = (int)min((p.places + kTile - 1) / kTile, (((long long)in.at.most << in.at.shift) + kTile - 1) / kTile);
+    int each = (tiles + in.splits - 1) / in.splits;
+    each = (each + step - 1) / step * step;
+    p.first = (int)min((long long)p.split * each, (long long)tiles);
+    p.end = min(p.first + each, tiles);
+    return p;
+}
+
+// The place of a tile whose key the lane `lane` holds in the first half of the first product's rows; 4 more in the second.
+__device__ inline int key_place(int lane) { return ((lane & 15) >> 2) * 8 + (lane & 3); }
+
+// The halves of words that hold values of places which are there: of the 8 places from first_place on.
+__device__ inline u32x4 held_fields(bool there, int first_place, long long places) {
+    u32x4 holds;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        holds[i] = (there && first_place + 2 * i < places ? 0xFFFFu : 0u) | (there && first_place + 2 * i + 1 < places ? 0xFFFF0000u : 0u);
+    return holds;
+}
+
+// Few columns: the four waves share them, take every fourth tile, and add up at the end.  Keys and values come from the cache into registers, the next
+// tile's as soon as this one's are used.
+template <class T, int KC, int NQ, bool EXACT>
+__global__ __launch_bounds__(kAttentionThreads) void attention_shared_kernel(AttentionIn in) {
+    constexpr int VT = KC * 2, STEP = 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, group = lane >> 4;
+    const int d = EXACT ? KC * 32 : in.at.d;
+    const Piece p = piece_of(in, NQ * 16, STEP);
+    if (p.nothing) return;
+    const int end = p.end, len = p.len;
+    Columns<T, KC, NQ, EXACT> cols;
+    cols.start(in, p.s, p.head, p.block * NQ * 16, p.count, in.parents ? tree_line(in, p.s, p.count, lane) : 0, d, lane);
+
+    const int* pages = in.at.pages + p.s * in.at.stride;
+    const long long page_values = in.at.page_values();
+    const int in_page = in.at.page() - 1;
+    const bool second_k = col >> 3, second_v = group >> 1;          // in the tile's second 16 places
+    const int k_lane = (key_place(lane) & 15) * d + group * 8, v_lane = (group & 1) * 8 * d + col * 8;
+    const T* const k_head = (const T*)in.k_cache + ((long long)p.head << in.at.shift) * d;
+    const T* const v_head = (const T*)in.v_cache + ((long long)p.head << in.at.shift) * d;
+    u32x4 keys[2][KC], values[VT];
+    const auto load_keys = [&](int tile, const TilePages& at) {
+        const int off0 = (tile * kTile) & in_page, off1 = (tile * kTile + 16) & in_page;
+        const T* from = k_head + (second_k ? max(at.second, 0) * page_values + off1 * d : max(at.first, 0) * page_values + off0 * d) + k_lane;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < KC; ++c) keys[t][c] = EXACT || c * 32 + group * 8 < d ? *reinterpret_cast<const u32x4*>(from + t * 4 * d + c * 32) : u32x4{};
+    };
+    const auto load_values = [&](int tile, const TilePages& at) {
+        const int off0 = (tile * kTile) & in_page, off1 = (tile * kTile + 16) & in_page;
+        const T* from = v_head + (second_v ? max(at.second, 0) * page_values + off1 * d : max(at.first, 0) * page_values + off0 * d) + v_lane;
+#pragma unroll
+        for (int v = 0; v < VT; ++v) values[v] = EXACT || v * 16 + col < d ? *reinterpret_cast<const u32x4*>(from + v * 128) : u32x4{};
+    };
+
+    int tile = p.first + wave;
+    TilePages now = tile_pages(in.at, pages, tile, end), next = tile_pages(in.at, pages, tile + STEP, end);
+    if (tile < end) {
+        load_keys(tile, now);
+        load_values(tile, now);
+    }
+    bool odd = false;
+    const auto go = [&](auto masked) {
+        constexpr bool MASKED = decltype(masked)::value;
+        const TilePages after = tile_pages(in.at, pages, tile + 2 * STEP, end);
+        const bool more = tile + STEP < end;
+        f32x4 score[NQ][2];
+        cols.settle();
+        cols.scores(keys, score);
+        if (more) load_keys(tile + STEP, next);
+        if constexpr (MASKED) {
+            const int first_place = tile * kTile + group * 8;
+            const bool there = second_v ? now.second >= 0 : now.first >= 0;
+            cols.mask(in, score, first_place, len, there);
+            odd |= cols.tame(values, held_fields(there, first_place, p.places));
+        }
+        cols.weigh_and_add(score, in.scale, values);
+        if (more) load_values(tile + STEP, next);
+        now = next, next = after;
         tile += STEP;
     };
     // tiles of places that every column sees, then those with rows, or (seldom) all from the first that lacks a page
     const int seen_by_all = min(end, len / kTile);
-    while (tile < seen_by_all && page0 >= 0 && page1 >= 0) go(std::false_type{});
+    while (tile < seen_by_all && now.both()) go(std::false_type{});
+    const int first_masked = tile;
     while (tile < end) go(std::true_type{});
+    if (__any(odd)) cols.add_odd(in, p.s, p.head, p.block * NQ * 16, first_masked, end, STEP, len, d, lane);
 
-    // a column's lanes hold sums of all its places, but each the total of its own 8 of every 32
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-        total[t] += __shfl_xor(total[t], 16);
-        total[t] += __shfl_xor(total[t], 32);
-        if (row[t] < 0) {                            // went along with the others over the tiles without a mask
-            total[t] = 0.f;
-            reference[t] = -INFINITY;
-#pragma unroll
-            for (int v = 0; v < VT; ++v) sums[t][v] = f32x4{};
-        }
-    }
-    if constexpr (!APART) {
-        // the waves' sums about the largest of their references, added up in a fixed order: 0 + 2, 1 + 3, then both
-        __shared__ float refs[4][NQ][16], totals[4][NQ][16];
-        __shared__ f32x4 shared[2][NQ][VT][64];
-        if (group == 0)
-#pragma unroll
-            for (int t = 0; t < NQ; ++t) {
-                refs[wave][t][col] = reference[t];
-                totals[wave][t][col] = total[t];
-            }
-        __syncthreads();
+    cols.finish();
+    // the waves' sums about the largest of their references, added up in a fixed order: 0 + 2, 1 + 3, then both
+    __shared__ float refs[4][NQ][16], totals[4][NQ][16];
+    __shared__ f32x4 shared[2][NQ][VT][64];
+    if (group == 0)
 #pragma unroll
         for (int t = 0; t < NQ; ++t) {
-            float most = -INFINITY, sum = 0.f;
-            for (int w = 0; w < 4; ++w) most = fmaxf(most, refs[w][t][col]);
-            for (int w = 0; w < 4; ++w) sum += refs[w][t][col] == -INFINITY ? totals[w][t][col] : totals[w][t][col] * (refs[w][t][col] == most ? 1.f : exp2_fast(refs[w][t][col] - most));
-            const float shrink = reference[t] == most || reference[t] == -INFINITY ? 1.f : exp2_fast(reference[t] - most);
-#pragma unroll
-            for (int v = 0; v < VT; ++v) sums[t][v] *= shrink;
-            reference[t] = most;
-            total[t] = sum;
+            refs[wave][t][col] = cols.reference[t];
+            totals[wave][t][col] = cols.total[t];
         }
-        if (wave >= 2)
-#pragma unroll
-            for (int t = 0; t < NQ; ++t)
-#pragma unroll
-                for (int v = 0; v < VT; ++v) shared[wave - 2][t][v][lane] = sums[t][v];
-        __syncthreads();
-        if (wave < 2)
-#pragma unroll
-            for (int t = 0; t < NQ; ++t)
-#pragma unroll
-                for (int v = 0; v < VT; ++v) sums[t][v] += shared[wave][t][v][lane];
-        __syncthreads();
-        if (wave == 1)
-#pragma unroll
-            for (int t = 0; t < NQ; ++t)
-#pragma unroll
-                for (int v = 0; v < VT; ++v) shared[0][t][v][lane] = sums[t][v];
-        __syncthreads();
-        if (wave != 0) return;
-#pragma unroll
-        for (int t = 0; t < NQ; ++t)
-#pragma unroll
-            for (int v = 0; v < VT; ++v) sums[t][v] += shared[0][t][v][lane];
-    }
-
+    __syncthreads();
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
-        const int x = first_col + t * 16 + col;
-        if (x >= all_cols) continue;
-        const int h = head * share + x % share;
-        const long long flat = s * m + x / share;
-        if (in.splits > 1) {
-            const long long at = (flat * in.heads + h) * in.splits + split;
-            if (group == 0) in.norms[at] = make_float2(reference[t], total[t]);
+        float most = -INFINITY, sum = 0.f;
+        for (int w = 0; w < 4; ++w) most = fmaxf(most, refs[w][t][col]);
+        for (int w = 0; w < 4; ++w) sum += totals[w][t][col] * shrink_by(refs[w][t][col], most);
+        const float shrink = shrink_by(cols.reference[t], most);
 #pragma unroll
-            for (int v = 0; v < VT; ++v) {
-                const int c = v * 16 + group * 4;
-                if (EXACT || c < d) *reinterpret_cast<f32x4*>(in.sums + at * d + c) = sums[t][v];
-            }
-        } else {
-            const float by = total[t] == 0.f ? 0.f : 1.f / total[t];
-            if (in.lse && group == 0) in.lse[flat * in.heads + h] = total[t] == 0.f ? -INFINITY : (reference[t] + __log2f(total[t])) * kLn2;
-            T* to = (T*)in.out + flat * in.out_stride + (long long)h * d + group * 4;
-#pragma unroll
-            for (int v = 0; v < VT; ++v)
-                if (EXACT || v * 16 + group * 4 < d) {
-                    typedef T v4 __attribute__((ext_vector_type(4)));
-                    v4 y;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) y[i] = (T)(sums[t][v][i] * by);
-                    *reinterpret_cast<v4*>(to + v * 16) = y;
-                }
-        }
+        for (int v = 0; v < VT; ++v) cols.sums[t][v] *= shrink;
+        cols.reference[t] = most;
+        cols.total[t] = sum;
     }
+    for (int half = 2; half >= 1; half /= 2) {
+        if (wave >= half && wave < 2 * half)
+#pragma unroll
+            for (int t = 0; t < NQ; ++t)
+#pragma unroll
+                for (int v = 0; v < VT; ++v) shared[wave - half][t][v][lane] = cols.sums[t][v];
+        __syncthreads();
+        if (wave < half)
+#pragma unroll
+            for (int t = 0; t < NQ; ++t)
+#pragma unroll
+                for (int v = 0; v < VT; ++v) cols.sums[t][v] += shared[wave][t][v][lane];
+        __syncthreads();
+    }
+    if (wave == 0) cols.write(in, p.s, p.head, p.split, p.block * NQ * 16, d, lane);
+}
+
+// Many columns: each wave has its own and goes over all tiles, which pass through the LDS.  A tile is 4 KC operands of a wave, 1 KB each in the order of
+// the lanes, so that they come and go in whole lines: 2 KC of keys, then 2 KC of values.  A wave brings KC of them: into registers three tiles
+// ahead, into the LDS one tile ahead.
+template <class T, int KC, int NQ, bool EXACT>
+__global__ __launch_bounds__(kAttentionThreads) void attention_tiles_kernel(AttentionIn in) {
+    constexpr int VT = KC * 2, PARTS = 4 * KC;
+    __shared__ u32x4 stage[2][PARTS][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, group = lane >> 4;
+    const int d = EXACT ? KC * 32 : in.at.d;
+    const Piece p = piece_of(in, NQ * 64, 1);
+    if (p.nothing) return;
+    const int end = p.end, len = p.len;
+    const int first_col = (p.block * 4 + wave) * NQ * 16;
+    Columns<T, KC, NQ, EXACT> cols;
+    cols.start(in, p.s, p.head, first_col, p.count, in.parents ? tree_line(in, p.s, p.count, lane) : 0, d, lane);
+
+    const int* pages = in.at.pages + p.s * in.at.stride;
+    const long long page_values = in.at.page_values();
+    const int in_page = in.at.page() - 1;
+    const bool for_values = wave >= 2;
+    const bool second = for_values ? group >> 1 : col >> 3;         // in the tile's second 16 places
+    const int from_lane = for_values ? (group & 1) * 8 * d + col * 8 + (wave - 2) * KC * 128 : (key_place(lane) & 15) * d + group * 8 + wave * 4 * d;
+    const T* const from_head = (const T*)(for_values ? in.v_cache : in.k_cache) + ((long long)p.head << in.at.shift) * d + from_lane;
+    const int apart = for_values ? 128 : 32;
+    struct Parts {
+        u32x4 of[KC];
+    };
+    const auto bring = [&](int tile, const TilePages& at, Parts& to) {
+        const int off0 = (tile * kTile) & in_page, off1 = (tile * kTile + 16) & in_page;
+        const T* from = from_head + (second ? max(at.second, 0) * page_values + off1 * d : max(at.first, 0) * page_values + off0 * d);
+#pragma unroll
+        for (int i = 0; i < KC; ++i) {
+            const bool some = EXACT || (for_values ? ((wave - 2) * KC + i) * 16 + col < d : i * 32 + group * 8 < d);
+            to.of[i] = some ? *reinterpret_cast<const u32x4*>(from + i * apart) : u32x4{};
+        }
+    };
+    const auto put = [&](int tile, const Parts& parts) {
+#pragma unroll
+        for (int i = 0; i < KC; ++i) stage[tile & 1][wave * KC + i][lane] = parts.of[i];
+    };
+    int tile = p.first;
+    TilePages now = tile_pages(in.at, pages, tile, end), next = tile_pages(in.at, pages, tile + 1, end), third = tile_pages(in.at, pages, tile + 2, end);
+    Parts ahead;                                     // the next tile's
+    if (tile < end) {
+        bring(tile, now, ahead);
+        put(tile, ahead);
+    }
+    if (tile + 1 < end) bring(tile + 1, next, ahead);
+    bool odd = false;
+    const auto go = [&](auto masked) {
+        constexpr bool MASKED = decltype(masked)::value;
+        __syncthreads();                             // this tile is there, and the other stage is free
+        const u32x4(*at)[64] = stage[tile & 1];
+        u32x4 keys[2][KC], values[VT];
+        cols.settle();
+#pragma unroll
+        for (int i = 0; i < 2 * KC; ++i) keys[i / KC][i % KC] = at[i][lane];
+        const TilePages after = tile_pages(in.at, pages, tile + 3, end);
+        if (tile + 1 < end) put(tile + 1, ahead);
+        if (tile + 2 < end) bring(tile + 2, third, ahead);
+        f32x4 score[NQ][2];
+        cols.scores(keys, score);
+#pragma unroll
+        for (int i = 0; i < VT; ++i) values[i] = at[2 * KC + i][lane];
+        if constexpr (MASKED) {
+            const int first_place = tile * kTile + group * 8;
+            const bool there = group >> 1 ? now.second >= 0 : now.first >= 0;
+            cols.mask(in, score, first_place, len, there);
+            odd |= cols.tame(values, held_fields(there, first_place, p.places));
+        }
+        cols.weigh_and_add(score, in.scale, values);
+        now = next, next = third, third = after;
+        ++tile;
+    };
+    const int seen_by_all = min(end, len / kTile);
+    while (tile < seen_by_all && now.both()) go(std::false_type{});
+    const int first_masked = tile;
+    while (tile < end) go(std::true_type{});
+    if (__any(odd)) cols.add_odd(in, p.s, p.head, first_col, first_masked, end, 1, len, d, lane);
+    cols.finish();
+    cols.write(in, p.s, p.head, p.split, first_col, d, lane);
 }
 
 // The parts of a row and head added up: a thread has 4 components of one of them.
@@ -400,7 +564,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionIn in, lon
     float total = 0.f;
     for (int p = 0; p < in.splits; ++p) {
         const float2 norm = in.norms[at * in.splits + p];
-        const float by = norm.x == most || norm.x == -INFINITY ? 1.f : exp2_fast(norm.x - most);
+        const float by = shrink_by(norm.x, most);
         total += norm.y * by;
         sum += *reinterpret_cast<const f32x4*>(in.sums + (at * in.splits + p) * d + c) * by;
     }
@@ -419,11 +583,12 @@ template <class T, int KC, bool EXACT>
 int launch_attention(const AttentionIn& in, const AttentionPlan& plan, hipStream_t stream) {
     const long long passes = in.n * in.at.kv_heads * in.splits;
     const dim3 grid((unsigned)((passes + 7) / 8 * 8 * in.blocks)), threads(kAttentionThreads);
-    constexpr int MOST = KC > 4 ? 2 : 4;
-    if (plan.apart) hipLaunchKernelGGL((attention_kernel<T, KC, MOST, true, EXACT>), grid, threads, 0, stream, in);
-    else if (plan.tiles == 1) hipLaunchKernelGGL((attention_kernel<T, KC, 1, false, EXACT>), grid, threads, 0, stream, in);
-    else if (plan.tiles == 2) hipLaunchKernelGGL((attention_kernel<T, KC, 2, false, EXACT>), grid, threads, 0, stream, in);
-    else if constexpr (MOST == 4) hipLaunchKernelGGL((attention_kernel<T, KC, 4, false, EXACT>), grid, threads, 0, stream, in);
+    constexpr int MOST = KC > 4 ? 2 : 4;             // tiles of columns whose sums fit a wave's registers
+    if (plan.apart && plan.tiles == 2) hipLaunchKernelGGL((attention_tiles_kernel<T, KC, 2, EXACT>), grid, threads, 0, stream, in);
+    else if (plan.apart) hipLaunchKernelGGL((attention_tiles_kernel<T, KC, MOST, EXACT>), grid, threads, 0, stream, in);
+    else if (plan.tiles == 1) hipLaunchKernelGGL((attention_shared_kernel<T, KC, 1, EXACT>), grid, threads, 0, stream, in);
+    else if (plan.tiles == 2) hipLaunchKernelGGL((attention_shared_kernel<T, KC, 2, EXACT>), grid, threads, 0, stream, in);
+    else if constexpr (MOST == 4) hipLaunchKernelGGL((attention_shared_kernel<T, KC, 4, EXACT>), grid, threads, 0, stream, in);
     HIP_TRY(hipGetLastError());
     if (in.splits > 1) {
         const long long pieces = in.n * in.at.m * in.heads * (in.at.d / 4);
@@ -491,7 +656,7 @@ int ivfpq_draft_attention(const void* d_q, int64_t q_stride, int32_t heads, int6
             if (workspace_bytes < need) return fail(IVFPQ_ENOSPACE, "%s: workspace %zu bytes, need %zu", what, workspace_bytes, need);
         }
         AttentionIn in{d_q, d_k_cache, d_v_cache, d_out, d_lse, (float*)d_workspace, nullptr, d_parents, q_stride, out_stride, n, heads, plan.blocks, plan.splits,
-                       (float)((double)scale * 1.4426950408889634), pages_in(d_pages, max_pages, d_lens, d_counts, n_pages, kv_heads, page, d, m)};
+                       (float)std::max(std::abs((double)scale) * 1.4426950408889634, 1e-37), scale < 0.f, pages_in(d_pages, max_pages, d_lens, d_counts, n_pages, kv_heads, page, d, m)};
         in.norms = (float2*)(in.sums + (size_t)rows * heads * plan.splits * d);      // d is a multiple of 8
         // max_places bounds what is looked at: the table's end does
         in.at.most = n_pages ? (int)std::min<int64_t>(max_pages, (max_places + page - 1) / page) : 0;

@@ -21,7 +21,7 @@ inline AttentionPlan attention_plan(int64_t n, int m, int heads, int kv_heads, i
     const int most = d > 128 ? 2 : 4;                               // tiles whose sums fit a wave's registers
     AttentionPlan p{};
     p.apart = columns > 16 * most;
-    p.tiles = columns <= 16 ? 1 : columns <= 32 ? 2 : most;
+    p.tiles = p.apart ? (columns <= 128 ? 2 : most) : columns <= 16 ? 1 : columns <= 32 ? 2 : most;
     p.blocks = (int)((columns + p.columns() - 1) / p.columns());
     // workgroups for every CU twice over, each of at least two tiles of places a wave
     const int64_t groups = n * kv_heads * p.blocks;

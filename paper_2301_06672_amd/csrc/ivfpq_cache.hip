@@ -176,52 +176,75 @@ struct KeepIn {
 
 constexpr int kKeepThreads = 256, kKeepBatch = 8;
 
-// A thread moves 8 components of a head through all kept rows.  The row that comes to place i lies at i or behind it and before the sources of later
-// places, so what a batch overwrites is never read by a later one; within a batch everything is read first.
+// Where a kept row lies and goes to: page, and place in the page.
+struct Move {
+    int from, from_place, to, to_place;
+};
+
+// A thread moves 8 components of a head in a layer through all kept rows.  The row that comes to place i lies behind it and before the sources of
+// later places, so what a batch overwrites is never read by a later one; within a batch everything is read first.  Where rows lie is looked up for the
+// whole workgroup at once, and rows that stay are left out, so that a batch is loaded without a branch.  Bound by the lines that values of single places
+// lie in, 8 times what moves.
 __global__ __launch_bounds__(kKeepThreads) void cache_keep_kernel(KeepIn in) {
-    const int d = in.at.d, m = in.at.m, pieces = d / 8, per = in.at.kv_heads * pieces;
+    __shared__ Move moves[kKeepThreads];
+    __shared__ int found[kKeepThreads / 64];
+    const int d = in.at.d, m = in.at.m, pieces = d / 8, per = in.at.kv_heads * pieces, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const long long s = blockIdx.y;
     const int kept = min(max(in.kept[s], 0), m);
     const long long len = in.at.len(s);
-    const long long i = (long long)blockIdx.x * kKeepThreads + threadIdx.x;
-    if (i >= (long long)per * in.layers) return;
-    const long long layer = i / per;
-    const int head = (int)(i % per) / pieces, c = (int)(i % per) % pieces * 8;
-    uint16_t* k = in.k_cache + layer * in.at.n_pages * in.at.page_values();
-    uint16_t* v = in.v_cache + layer * in.at.n_pages * in.at.page_values();
+    const unsigned i = blockIdx.x * kKeepThreads + tid;         // under 2^32: 2^12 layers of 2^12 heads of 2^5 pieces at most
+    const bool mine = i < (unsigned)per * in.layers;
+    const unsigned layer = mine ? i / per : 0, rest = mine ? i - layer * per : 0, head = rest / pieces, c = rest % pieces * 8;
+    const long long layer_base = layer * (in.at.n_pages * in.at.page_values());
+    const long long head_base = ((long long)head << in.at.shift) * d;
+    uint16_t* const keys_at = in.k_cache + layer_base + head_base + c;
+    uint16_t* const values_at = in.v_cache + layer_base + head_base + c * 8;
     const int* path = in.path + s * m;
-    const long long head_base = (long long)head << in.at.shift;
     const int in_page = in.at.page() - 1;
-    for (int at = 0; at < kept; at += kKeepBatch) {
-        uint4 keys[kKeepBatch];
-        uint16_t values[kKeepBatch][8];
-        int target[kKeepBatch];                      // the page of the place it goes to, -1: nothing moves
-#pragma unroll
-        for (int j = 0; j < kKeepBatch; ++j) {
-            target[j] = -1;
-            if (at + j >= kept) continue;
-            const int row = path[at + j];
-            if (row <= at + j || row >= m) continue; // in place already, or no row of the pass
-            const int page = in.at.page_of(s, len + row);
-            if (page < 0) continue;
-            target[j] = in.at.page_of(s, len + at + j);
-            if (target[j] < 0) continue;
-            const int off = (int)(len + row) & in_page;
-            const long long from = (long long)page * in.at.page_values();
-            keys[j] = *reinterpret_cast<const uint4*>(k + from + (head_base + off) * d + c);
-            const uint16_t* x = v + from + (head_base + (off & ~7)) * d + c * 8 + (off & 7);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) values[j][e] = x[e * 8];
+    for (int base = 0; base < kept; base += kKeepThreads) {
+        Move move{-1, 0, -1, 0};
+        if (base + tid < kept) {
+            const int row = path[base + tid];
+            if (row > base + tid && row < m) {
+                move = Move{in.at.page_of(s, len + row), (int)(len + row) & in_page, in.at.page_of(s, len + base + tid), (int)(len + base + tid) & in_page};
+            }
         }
+        const bool moves_so = move.from >= 0 && move.to >= 0;
+        const uint64_t mask = __ballot(moves_so);
+        __syncthreads();                                        // of the rows before
+        if (lane == 0) found[wave] = __popcll(mask);
+        __syncthreads();
+        int count = 0, at = 0;
 #pragma unroll
-        for (int j = 0; j < kKeepBatch; ++j) {
-            if (target[j] < 0) continue;
-            const int off = (int)(len + at + j) & in_page;
-            const long long to = (long long)target[j] * in.at.page_values();
-            *reinterpret_cast<uint4*>(k + to + (head_base + off) * d + c) = keys[j];
-            uint16_t* y = v + to + (head_base + (off & ~7)) * d + c * 8 + (off & 7);
+        for (int w = 0; w < kKeepThreads / 64; ++w) {
+            if (w == wave) at = count + __popcll(mask & (((uint64_t)1 << lane) - 1));
+            count += found[w];
+        }
+        if (moves_so) moves[at] = move;
+        __syncthreads();
+        if (!mine) continue;
+        for (int first = 0; first < count; first += kKeepBatch) {
+            uint4 keys[kKeepBatch];
+            uint16_t values[kKeepBatch][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e * 8] = values[j][e];
+            for (int j = 0; j < kKeepBatch; ++j) {
+                const Move x = moves[min(first + j, count - 1)];
+                const long long from = x.from * in.at.page_values();
+                keys[j] = *reinterpret_cast<const uint4*>(keys_at + from + x.from_place * d);
+                const uint16_t* v = values_at + from + (x.from_place & ~7) * d + (x.from_place & 7);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) values[j][e] = v[e * 8];
+            }
+#pragma unroll
+            for (int j = 0; j < kKeepBatch; ++j) {
+                if (first + j >= count) break;
+                const Move x = moves[first + j];
+                const long long to = x.to * in.at.page_values();
+                *reinterpret_cast<uint4*>(keys_at + to + x.to_place * d) = keys[j];
+                uint16_t* v = values_at + to + (x.to_place & ~7) * d + (x.to_place & 7);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e * 8] = values[j][e];
+            }
         }
     }
 }

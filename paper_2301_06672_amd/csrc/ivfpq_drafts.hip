@@ -46,13 +46,13 @@ __global__ __launch_bounds__(THREADS) void neighbour_drafts_kernel(DraftsIn in, 
     __shared__ int tokens[ROOM], parents[ROOM];                                  // a parent: the low 14 bits of its key, or -1
     __shared__ u64 best_keys[kMostNodes];
     __shared__ int best_tokens[kMostNodes], best_parents[kMostNodes], names[kMostNodes];
-    __shared__ int listed, counts[2];
+    __shared__ int texts[IVFPQ_MAX_DRAFT_DEPTH][K];
+    __shared__ int listed, counts[3];
     __shared__ u64 sums[WAVES];
     __shared__ float scratch[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, k = in.k, nodes = in.m - 1;
     const long long q = blockIdx.x;
 
-    long long at[EACH];                // where a neighbour's continuation goes on
     int token[EACH], group[EACH];
     u64 weight[EACH];                  // 0: follows no further
     float dist[EACH];
@@ -62,13 +62,17 @@ __global__ __launch_bounds__(THREADS) void neighbour_drafts_kernel(DraftsIn in, 
         const int j = i * THREADS + tid;
         dist[i] = INFINITY;
         token[i] = -1;
-        at[i] = 0;
         if (j < k) {
             const long long id = in.ids[q * k + j];
             const float d = in.dists[q * k + j];
             if (id >= 0 && id < in.n_ids && fabsf(d) < INFINITY) {
-                at[i] = id;
-                token[i] = in.text[id];
+                // the whole continuation, so that the way down waits for memory once
+                int words[IVFPQ_MAX_DRAFT_DEPTH];
+#pragma unroll
+                for (int t = 0; t < IVFPQ_MAX_DRAFT_DEPTH; ++t) words[t] = t < in.depth && id + t < in.n_ids ? in.text[id + t] : -1;
+#pragma unroll
+                for (int t = 1; t < IVFPQ_MAX_DRAFT_DEPTH; ++t) texts[t][j] = words[t];
+                token[i] = words[0];
                 if (token[i] >= 0) dist[i] = d;
             }
         }
@@ -85,33 +89,43 @@ __global__ __launch_bounds__(THREADS) void neighbour_drafts_kernel(DraftsIn in, 
     }
     total = block_sum<THREADS>(total, sums);
 
-    // Keeps the `nodes` largest keys of the list, in any order.
+    // Keeps the `nodes` largest keys of the list, in any order; -> a number that so many keys are not under.  Bit by bit from the top, until the
+    // number parts the keys.
     const auto prune = [&] {
+        constexpr int HELD = ROOM / THREADS;
         const int n = listed;
-        u64 least = 0;                               // the largest number that so many keys are not under
-        int round = 0;
-        if (tid < 2) counts[tid] = 0;
+        u64 mine[HELD];
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) mine[i] = i * THREADS + tid < n ? keys[i * THREADS + tid] : 0;
+        u64 least = 0;
+        if (tid < 3) counts[tid] = 0;
         __syncthreads();
+        int round = 0;
         for (int bit = 56; bit >= 0; --bit) {
             const u64 probe = least | 1ull << bit;
             int over = 0;
-            for (int i = tid; i < n; i += THREADS) over += keys[i] >= probe;
-            for (int off = 32; off; off >>= 1) over += __shfl_xor(over, off);
-            if (lane == 0) atomicAdd(&counts[round & 1], over);
-            __syncthreads();
-            if (counts[round & 1] >= nodes) least = probe;
-            if (tid == 0) counts[(round + 1) & 1] = 0;
-            __syncthreads();
-            ++round;
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) over += __popcll(__ballot(mine[i] >= probe));
+            if constexpr (WAVES > 1) {               // counts of three rounds: one is added up, one read, one cleared for the next
+                if (lane == 0) atomicAdd(&counts[round], over);
+                if (tid == 0) counts[round == 2 ? 0 : round + 1] = 0;
+                __syncthreads();
+                over = counts[round];
+                round = round == 2 ? 0 : round + 1;
+            }
+            if (over >= nodes) least = probe;
+            if (over == nodes) break;
         }
+        __syncthreads();
         if (tid == 0) listed = 0;
         __syncthreads();
-        for (int i = tid; i < n; i += THREADS)
-            if (keys[i] >= least) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+            if (mine[i] >= least && mine[i] != 0) {
                 const int to = atomicAdd(&listed, 1);
-                best_keys[to] = keys[i];
-                best_tokens[to] = tokens[i];
-                best_parents[to] = parents[i];
+                best_keys[to] = mine[i];
+                best_tokens[to] = tokens[i * THREADS + tid];
+                best_parents[to] = parents[i * THREADS + tid];
             }
         __syncthreads();
         for (int i = tid; i < listed; i += THREADS) {
@@ -151,13 +165,6 @@ __global__ __launch_bounds__(THREADS) void neighbour_drafts_kernel(DraftsIn in, 
             atomicAdd(&weights[here], weight[i]);
         }
         __syncthreads();
-        // the next tokens are on their way while the nodes are listed
-        int next[EACH];
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            next[i] = -1;
-            if (weight[i] && t + 1 < in.depth && at[i] + 1 < in.n_ids) next[i] = in.text[at[i] + 1];
-        }
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             if (!weight[i]) continue;
@@ -179,9 +186,8 @@ __global__ __launch_bounds__(THREADS) void neighbour_drafts_kernel(DraftsIn in, 
         if (listed > ROOM - K) least = prune();
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            token[i] = next[i];
-            at[i] += 1;
-            if (next[i] < 0) weight[i] = 0;
+            token[i] = weight[i] && t + 1 < in.depth ? texts[t + 1][i * THREADS + tid] : -1;
+            if (token[i] < 0) weight[i] = 0;
         }
     }
     __syncthreads();

@@ -25,6 +25,12 @@ struct BlockSum {
     int unused;
 };
 
+// What a row says: its token (-1: none) and the logarithm of its probability.
+struct Said {
+    int token;
+    float chance;
+};
+
 struct VerifyIn {
     const void *logits, *drafts;
     long long stride, draft_stride;
@@ -33,6 +39,7 @@ struct VerifyIn {
     BlockSum* blocks;                                 // [n * m + n * (m - 1) with drafts][row_blocks]
     double* left;                                     // drafts: [n][left_blocks]
     struct Stop* stops;                               // drafts: [n]
+    Said* said;                                       // without drafts: [n * m]
     int *path, *kept, *next;
     float* logprobs;
     long long n;
@@ -69,20 +76,63 @@ __device__ inline double exp2_exact(double y) {
     p = fma(p, f, 1.0);
     return __builtin_amdgcn_ldexp(p, (int)n);
 }
+// The same for -1023 < y <= 0.  The nearest whole number comes from an addition that leaves it in the low bits.
+// The coefficients stay in vector registers: an operation takes one from a scalar register at most, and a copy of it costs as much as half of one.
+struct Exp2Terms {
+    double c[9] = {1.0, 0x1.62e42fef84cf0p-1, 0x1.ebfbdff823cedp-3, 0x1.c6b08dd6fd236p-5, 0x1.3b2ab7181b778p-7, 0x1.5d8745a72827ap-10, 0x1.4308ac85a6c21p-13,
+                   0x1.00dc4a534054dp-16, 0x1.63d1363a7ecb6p-20};
+    __device__ inline Exp2Terms() {
+#pragma unroll
+        for (int i = 0; i < 9; ++i) asm("" : "+v"(c[i]));
+    }
+    __device__ inline double operator()(double y) const {
+        constexpr double kWhole = 0x1.8p52;
+        const double shifted = y + kWhole, f = y - (shifted - kWhole);
+        double p = c[8];
+#pragma unroll
+        for (int i = 7; i >= 0; --i) p = fma(p, f, c[i]);
+        return __builtin_amdgcn_ldexp(p, __builtin_bit_cast(int2, shifted).x);
+    }
+};
 // exp((x - most) / T); `most` is finite
 __device__ inline double weight(float x, float most, double scale) { return exp2_exact(((double)x - (double)most) * scale); }
 
-__device__ inline double wave_sum(double x) {
-    for (int off = 32; off; off >>= 1) x += __shfl_xor(x, off);
-    return x;
+// x of another lane by the data paths between lanes, `none` where that lane does not exist (a step of a scan)
+template <int CTRL, int ROWS>
+__device__ inline int other_lane(int none, int x) { return __builtin_amdgcn_update_dpp(none, x, CTRL, ROWS, 0xF, false); }
+template <int CTRL, int ROWS>
+__device__ inline double plus_other_lane(double x) {
+    const int2 bits = __builtin_bit_cast(int2, x);
+    return x + __builtin_bit_cast(double, make_int2(other_lane<CTRL, ROWS>(0, bits.x), other_lane<CTRL, ROWS>(0, bits.y)));
 }
-// the sum over the lanes up to this one
+// the sum over the lanes up to this one: within rows of 16 lanes by shifts of 1, 2, 4 and 8, then the last lanes of rows spread to the rows behind
 __device__ inline double wave_scan(double x) {
-    for (int off = 1; off < 64; off <<= 1) {
-        const double below = __shfl_up(x, off);
-        if ((int)(threadIdx.x & 63) >= off) x += below;
-    }
-    return x;
+    x = plus_other_lane<0x111, 0xF>(x);
+    x = plus_other_lane<0x112, 0xF>(x);
+    x = plus_other_lane<0x114, 0xF>(x);
+    x = plus_other_lane<0x118, 0xF>(x);
+    x = plus_other_lane<0x142, 0xA>(x);
+    return plus_other_lane<0x143, 0xC>(x);
+}
+__device__ inline double from_lane(double x, int lane) {
+    const int2 bits = __builtin_bit_cast(int2, x);
+    return __builtin_bit_cast(double, make_int2(__builtin_amdgcn_readlane(bits.x, lane), __builtin_amdgcn_readlane(bits.y, lane)));
+}
+__device__ inline double wave_sum(double x) { return from_lane(wave_scan(x), 63); }
+template <int CTRL, int ROWS>
+__device__ inline float most_of_lanes(float x) {
+    const float other = __int_as_float(other_lane<CTRL, ROWS>(__float_as_int(x), __float_as_int(x)));
+    return maximum3(x, other, other);
+}
+// NaN if one is
+__device__ inline float wave_maximum(float x) {
+    x = most_of_lanes<0x111, 0xF>(x);
+    x = most_of_lanes<0x112, 0xF>(x);
+    x = most_of_lanes<0x114, 0xF>(x);
+    x = most_of_lanes<0x118, 0xF>(x);
+    x = most_of_lanes<0x142, 0xA>(x);
+    x = most_of_lanes<0x143, 0xC>(x);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 __device__ inline bool bad_most(float most) { return !(most < INFINITY); }       // NaN or +inf in the row
 
@@ -119,15 +169,16 @@ template <class T>
 __global__ __launch_bounds__(kSumThreads) void block_sums_kernel(VerifyIn in) {
     constexpr int VEC = Chunk<T>::VEC;
     const int lane = threadIdx.x & 63;
-    const long long item = (long long)blockIdx.x * (kSumThreads / 64) + (threadIdx.x >> 6);
-    const long long row = item / in.row_blocks, targets = in.n * in.m;
-    const int block = (int)(item % in.row_blocks);
+    // 2^25 blocks of 2^21 rows at most; divisions of 64 bits would take as long as a third of the sums
+    const unsigned item = __builtin_amdgcn_readfirstlane(blockIdx.x * (kSumThreads / 64) + (threadIdx.x >> 6));
+    const unsigned row = item / (unsigned)in.row_blocks, targets = (unsigned)(in.n * in.m);
+    const int block = (int)(item - row * in.row_blocks);
     const bool draft = row >= targets;
-    const long long r = draft ? row - targets : row;
-    if (draft && (!in.drafts || r >= in.n * (in.m - 1))) return;
-    const int per = draft ? in.m - 1 : in.m;
+    const unsigned r = draft ? row - targets : row, per = draft ? in.m - 1 : in.m;
+    if (draft && (!in.drafts || r >= (unsigned)in.n * per)) return;
+    const unsigned s = r / per;
     // a draft row is used if the row that it drafted is
-    if ((int)(r % per) + (draft ? 1 : 0) >= in.count(r / per)) return;
+    if ((int)(r - s * per) + (draft ? 1 : 0) >= in.count(s)) return;
     const RowChunks<T> values(draft ? in.drafts : in.logits, r, draft ? in.draft_stride : in.stride, in.vocab);
     if (block * kBlock >= values.end) return;
     BlockChunks<T> held(values, block, lane);
@@ -140,22 +191,31 @@ __global__ __launch_bounds__(kSumThreads) void block_sums_kernel(VerifyIn in) {
         for (int e = 0; e < VEC; e += 2) most = maximum3(most, x[e], x[e + 1]);
         held.chunk[i].forget_widened();
     }
-    for (int off = 32; off; off >>= 1) {
-        const float other = __shfl_xor(most, off);
-        most = maximum3(most, other, other);
-    }
+    most = wave_maximum(most);
     double sum = 0.0;
     if (most > -INFINITY && most < INFINITY) {
+        const Exp2Terms power;
+        const auto add_up = [&](auto&& exponent) {
+            double sums[2] = {0.0, 0.0};
 #pragma unroll
-        for (int i = 0; i < held.N; ++i) {
-            float x[VEC];
-            held.chunk[i].widen(x);
+            for (int i = 0; i < held.N; ++i) {
+                float x[VEC];
+                held.chunk[i].widen(x);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) sum += weight(x[e], most, in.scale);
-        }
-        sum = wave_sum(sum);
+                for (int e = 0; e < VEC; ++e) sums[e & 1] += power(exponent(x[e]));
+            }
+            return wave_sum(sums[0] + sums[1]);
+        };
+        const double less = (double)most * in.scale;
+        if (fabs(less) < 0x1p30) {
+            // x scale - most scale in one operation; what the second product loses, under 2^-23, is a factor of the whole block.  What is under 2^-1000,
+            // of a logit of -inf too, is taken for that: lost in a sum that holds a 1
+            const float least = (float)((double)most - 1000.0 / in.scale);
+            const double lost = fma((double)most, in.scale, -less) * 0.6931471805599453;
+            sum = add_up([&](float x) { return fma((double)fmaxf(x, least), in.scale, -less); }) * (1.0 - lost + 0.5 * lost * lost);
+        } else sum = add_up([&](float x) { return fmax(((double)x - (double)most) * in.scale, -1000.0); });
     }
-    if (lane == 0) in.blocks[row * in.row_blocks + block] = BlockSum{sum, most, 0};
+    if (lane == 0) in.blocks[item] = BlockSum{sum, most, 0};
 }
 
 // A row's largest logit and the sum about it, from its blocks; the same in every lane.
@@ -163,18 +223,18 @@ struct Norm {
     float most;
     double total;                                     // 0: all -inf; NaN: bad
 };
+__device__ inline double block_weight(const BlockSum& b, float most, double scale) { return b.most > -INFINITY ? b.sum * weight(b.most, most, scale) : 0.0; }
+
 __device__ inline Norm row_norm(const BlockSum* blocks, int count, double scale, int lane) {
-    float most = -INFINITY;
-    for (int b = lane; b < count; b += 64) most = maximum3(most, blocks[b].most, blocks[b].most);
-    for (int off = 32; off; off >>= 1) {
-        const float other = __shfl_xor(most, off);
-        most = maximum3(most, other, other);
-    }
+    BlockSum mine{0.0, -INFINITY, 0};                 // of the first 64; a larger vocabulary's others are read twice
+    if (lane < count) mine = blocks[lane];
+    float most = mine.most;
+    for (int b = lane + 64; b < count; b += 64) most = maximum3(most, blocks[b].most, blocks[b].most);
+    most = wave_maximum(most);
     if (bad_most(most)) return Norm{most, NAN};
     if (most == -INFINITY) return Norm{most, 0.0};
-    double total = 0.0;
-    for (int b = lane; b < count; b += 64)
-        if (blocks[b].most > -INFINITY) total += blocks[b].sum * weight(blocks[b].most, most, scale);
+    double total = block_weight(mine, most, scale);
+    for (int b = lane + 64; b < count; b += 64) total += block_weight(blocks[b], most, scale);
     return Norm{most, wave_sum(total)};
 }
 
@@ -182,101 +242,74 @@ __device__ inline double unit(float u) {              // into [0, 1)
     return (double)fminf(fmaxf(u, 0.f), 0x1.fffffep-1f);
 }
 
-// The first block of `count` whose running sum, `of` it, is over `share` times the sum of all; `before`: the sum of those before it.  -1 if all are 0.
-template <class Of>
-__device__ inline int pick_block(int count, double share, int lane, double& before, Of&& of, double& all) {
-    all = 0.0;
-    for (int b = lane; b < count; b += 64) all += of(b);
-    all = wave_sum(all);
-    if (!(all > 0.0)) return -1;
-    const double target = share * all;
-    double base = 0.0;
-    int last = -1;                                    // the last block that is not 0: what rounding may leave over falls there
-    double last_base = 0.0;
-    for (int first = 0; first < count; first += 64) {
-        const int b = first + lane;
-        const double mine = b < count ? of(b) : 0.0;
-        const double upto = base + wave_scan(mine);
-        const uint64_t over = __ballot(mine > 0.0 && upto > target);
-        const uint64_t some = __ballot(mine > 0.0);
-        if (over) {
-            const int l = __ffsll((unsigned long long)over) - 1;
-            before = l ? __shfl(upto, l - 1) : base;
-            return first + l;
-        }
-        if (some) {
-            const int l = 63 - __clzll((long long)some);
-            last = first + l;
-            last_base = l ? __shfl(upto, l - 1) : base;
-        }
-        base = __shfl(upto, 63);
-    }
-    before = last_base;
-    return last;
+// Running sums over the lanes: the first lane at which one that adds something is over `target`, or else the last that adds something; -1 if none does.
+// before: the running sum before that lane.  base: the sum before the lanes, and after the call behind them.
+struct Crossing {
+    int lane;
+    bool over;
+    double before;
+};
+__device__ inline Crossing cross(double mine, double target, double& base) {
+    const double upto = base + wave_scan(mine);
+    const uint64_t some = __ballot(mine > 0.0), over = __ballot(mine > 0.0 && upto > target);
+    Crossing c{over ? __ffsll((unsigned long long)over) - 1 : some ? 63 - __clzll((long long)some) : -1, over != 0, base};
+    if (c.lane > 0) c.before = from_lane(upto, __builtin_amdgcn_readfirstlane(c.lane) - 1);
+    base = from_lane(upto, 63);
+    return c;
 }
 
-// The lowest token of a block whose running sum, with `before`, is over `target`; `by` times a value's weight is what it adds.
-template <class T>
-__device__ inline int pick_in_block(const RowChunks<T>& row, int block, float most, double scale, double by, double before, double target, int lane, float& logit) {
-    constexpr int VEC = Chunk<T>::VEC;
-    BlockChunks<T> held(row, block, lane);
-    double base = before;
-    int last = -1;
-    float last_logit = 0.f;
-#pragma unroll 1
-    for (int i = 0; i < held.N; ++i) {
-        // chunk i in a loop that is not unrolled: by a chain of selections
-        Chunk<T> chunk = held.chunk[0];
-#pragma unroll
-        for (int j = 1; j < held.N; ++j)
-            if (i == j) chunk = held.chunk[j];
-        float x[VEC];
-        chunk.widen(x);
-        double w[VEC], mine = 0.0;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            w[e] = by * weight(x[e], most, scale);
-            mine += w[e];
+// The first block of `count` whose running sum, `of` it, is over `share` times the sum of all.  -1 if all are 0.
+struct Picked {
+    int block;
+    double before, target;
+};
+template <class Of>
+__device__ inline Picked pick_block(int count, double share, int lane, Of&& of) {
+    const double mine = lane < count ? of(lane) : 0.0;
+    double all = mine;
+    for (int b = lane + 64; b < count; b += 64) all += of(b);
+    all = wave_sum(all);
+    Picked picked{-1, 0.0, share * all};
+    double base = 0.0;
+    for (int first = 0; first < count && all > 0.0; first += 64) {
+        const Crossing c = cross(first == 0 ? mine : first + lane < count ? of(first + lane) : 0.0, picked.target, base);
+        if (c.lane >= 0) {
+            picked.block = first + c.lane;
+            picked.before = c.before;
         }
-        const double upto = base + wave_scan(mine);
-        double at = __shfl_up(upto, 1);
-        if (lane == 0) at = base;
-        int found = -1, filled = -1;
-        float found_logit = 0.f, filled_logit = 0.f;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            at += w[e];
-            if (w[e] > 0.0) {
-                filled = e;
-                filled_logit = x[e];
-                if (found < 0 && at > target) {
-                    found = e;
-                    found_logit = x[e];
-                }
-            }
-        }
-        const int first = (block * (kBlock / VEC) + i * 64) * VEC - row.lead;
-        const uint64_t over = __ballot(found >= 0), some = __ballot(filled >= 0);
-        if (over) {
-            const int l = __ffsll((unsigned long long)over) - 1;
-            logit = __shfl(found_logit, l);
-            return first + l * VEC + __shfl(found, l);
-        }
-        if (some) {
-            const int l = 63 - __clzll((long long)some);
-            last = first + l * VEC + __shfl(filled, l);
-            last_logit = __shfl(filled_logit, l);
-        }
-        base = __shfl(upto, 63);
+        if (c.over) break;
     }
-    logit = last_logit;
-    return last;
+    return picked;
+}
+
+// The lowest of a block's tokens whose running sum, with what is before the block, is over the target; -1 if all weigh nothing.  A lane has
+// kLaneValues tokens in a row: their weights w, that lie from token `first` of the row on.
+__device__ inline int pick_token(const double (&w)[kLaneValues], int first, const Picked& picked) {
+    double mine = 0.0;
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) mine += w[i];
+    double base = picked.before;
+    const Crossing c = cross(mine, picked.target, base);
+    if (c.lane < 0) return -1;
+    double at = c.before;
+    int token = -1;
+    bool over = false;
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) {
+        at += w[i];
+        if (w[i] > 0.0 && !over) {
+            token = first + i;                        // the last one, where rounding leaves all under the target
+            over = at > picked.target;
+        }
+    }
+    return __builtin_amdgcn_readlane(token, __builtin_amdgcn_readfirstlane(c.lane));
 }
 
 // The token that a row's distribution has at the share u of its sum, or its most likely one; -1 without a distribution.
 template <class T>
 __device__ inline int draw(const VerifyIn& in, long long flat, const Norm& norm, bool greedy, double u, int lane, float& logit) {
     if (!(norm.total > 0.0)) return -1;
+    constexpr int VEC = Chunk<T>::VEC;
     const RowChunks<T> row(in.logits, flat, in.stride, in.vocab);
     const BlockSum* blocks = in.blocks + flat * in.row_blocks;
     const int count = (row.end + kBlock - 1) / kBlock;
@@ -289,21 +322,34 @@ __device__ inline int draw(const VerifyIn& in, long long flat, const Norm& norm,
         int token = 0x7FFFFFFF;
 #pragma unroll
         for (int i = 0; i < held.N; ++i) {
-            float x[Chunk<T>::VEC];
+            float x[VEC];
             held.chunk[i].widen(x);
 #pragma unroll
-            for (int e = 0; e < Chunk<T>::VEC; ++e)
-                if (x[e] == norm.most) token = min(token, (block * (kBlock / Chunk<T>::VEC) + i * 64 + lane) * Chunk<T>::VEC + e - row.lead);
+            for (int e = 0; e < VEC; ++e)
+                if (x[e] == norm.most) token = min(token, (block * (kBlock / VEC) + i * 64 + lane) * VEC + e - row.lead);
         }
         for (int off = 32; off; off >>= 1) token = min(token, __shfl_xor(token, off));
         logit = norm.most;
         return token;
     }
-    double before, all;
-    const auto of = [&](int b) { return blocks[b].most > -INFINITY ? blocks[b].sum * weight(blocks[b].most, norm.most, in.scale) : 0.0; };
-    const int block = pick_block(count, u, lane, before, of, all);
-    if (block < 0) return -1;
-    return pick_in_block<T>(row, block, blocks[block].most, in.scale, weight(blocks[block].most, norm.most, in.scale), before, u * all, lane, logit);
+    const Picked picked = pick_block(count, u, lane, [&](int b) { return block_weight(blocks[b], norm.most, in.scale); });
+    if (picked.block < 0) return -1;
+    const float most = blocks[picked.block].most;
+    const double by = weight(most, norm.most, in.scale);
+    const int first = picked.block * (kBlock / VEC) + lane * (kLaneValues / VEC);       // the lane's chunks lie in a row
+    double w[kLaneValues];
+#pragma unroll
+    for (int i = 0; i < kLaneValues / VEC; ++i) {
+        float x[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[e] = -INFINITY;
+        if (first + i < row.count()) row.load(first + i).widen(x);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) w[i * VEC + e] = by * weight(x[e], most, in.scale);
+    }
+    const int token = pick_token(w, first * VEC - row.lead, picked);
+    if (token >= 0) logit = row.value(token);
+    return token;
 }
 
 __device__ inline float log_probability(float logit, const Norm& norm, double scale) {
@@ -317,53 +363,53 @@ __device__ inline int row_block_count(const VerifyIn& in, const void* data, long
     return (RowChunks<T>(data, r, stride, in.vocab).end + kBlock - 1) / kBlock;
 }
 
-constexpr int kWalkThreads = 1024;
-
-// Drafts that were not drawn: a workgroup a sequence, whose waves draw the tokens of all rows; then the way through the tree, a row a lane.
+// The tokens of all used rows, a wave a row.
 template <class T>
-__global__ __launch_bounds__(kWalkThreads) void verify_tree_kernel(VerifyIn in) {
-    __shared__ int said[kMostDraft];
-    __shared__ float chances[kMostDraft];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = in.m;
+__global__ __launch_bounds__(64) void draw_rows_kernel(VerifyIn in) {
+    const int lane = threadIdx.x;
+    const long long flat = blockIdx.x, s = flat / in.m;
+    if ((int)(flat - s * in.m) >= in.count(s)) return;
+    const Norm norm = row_norm(in.blocks + flat * in.row_blocks, row_block_count<T>(in, in.logits, flat, in.stride), in.scale, lane);
+    float logit = 0.f;
+    const int token = draw<T>(in, flat, norm, !in.uniforms, in.uniforms ? unit(in.uniforms[flat]) : 0.0, lane, logit);
+    if (lane == 0) in.said[flat] = Said{token, token < 0 ? no_probability(norm) : log_probability(logit, norm, in.scale)};
+}
+
+// The way through a tree, a wave a sequence and a lane a row.
+__global__ __launch_bounds__(64) void verify_tree_kernel(VerifyIn in) {
+    const int lane = threadIdx.x, m = in.m;
     const long long s = blockIdx.x;
     const int count = in.count(s);
-    for (int i = wave; i < count; i += kWalkThreads / 64) {
-        const long long flat = s * m + i;
-        const Norm norm = row_norm(in.blocks + flat * in.row_blocks, row_block_count<T>(in, in.logits, flat, in.stride), in.scale, lane);
-        float logit = 0.f;
-        const int token = draw<T>(in, flat, norm, !in.uniforms, in.uniforms ? unit(in.uniforms[flat]) : 0.0, lane, logit);
-        if (lane == 0) {
-            said[i] = token;
-            chances[i] = token < 0 ? no_probability(norm) : log_probability(logit, norm, in.scale);
-        }
-    }
-    __syncthreads();
-    if (wave != 0) return;
     int up = -1, token = -1;
+    Said said{-1, -INFINITY};
     if (lane < count) {
         up = in.parents ? in.parents[s * m + lane] : lane - 1;
         if (up >= lane) up = -1;
         token = in.tokens[s * m + lane];
+        said = in.said[s * m + lane];
     }
     int kept = 0, at = 0, following = -1;
     int my_row = -1;                                  // of the path, at place `lane`
     while (kept < count) {                            // a child comes behind its parent
         if (lane == kept) my_row = at;
         ++kept;
-        following = said[at];
+        following = __shfl(said.token, at);
         const uint64_t children = __ballot(lane > 0 && lane < count && up == at && token == following && following >= 0);
         if (!children) break;
         at = __ffsll((unsigned long long)children) - 1;
     }
+    const float chance = __shfl(said.chance, max(my_row, 0));
     if (lane < m) {
         in.path[s * m + lane] = my_row;
-        in.logprobs[s * m + lane] = my_row >= 0 ? chances[my_row] : -INFINITY;
+        in.logprobs[s * m + lane] = my_row >= 0 ? chance : -INFINITY;
     }
     if (lane == 0) {
         in.kept[s] = kept;
         in.next[s] = following;
     }
 }
+
+constexpr int kWalkThreads = 1024;
 
 // A student's chain: which rows are kept, and the row where it ends.  A workgroup a sequence, a wave a row.
 template <class T>
@@ -424,12 +470,22 @@ __global__ __launch_bounds__(kWalkThreads) void verify_chain_kernel(VerifyIn in)
     }
 }
 
-// max(p - q, 0) of a token of the row where a chain ends
-template <class T>
-__device__ inline double left_of(const Stop& stop, const T* logits, const T* drafts, int token, double scale) {
-    const double p = weight((float)logits[token], stop.most, scale) / stop.total;
-    const double q = weight((float)drafts[token], stop.draft_most, scale) / stop.draft_total;
-    return fmax(p - q, 0.0);
+// max(p - q, 0) of kLaneValues tokens, STEP apart, of the row where a chain ends; 0 behind the vocabulary
+template <int STEP, class T>
+__device__ inline void left_weights(const Stop& stop, const T* logits, const T* drafts, int first, const VerifyIn& in, double (&w)[kLaneValues]) {
+    const double of_p = 1.0 / stop.total, of_q = 1.0 / stop.draft_total;
+    T x[kLaneValues], y[kLaneValues];
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) {
+        const int token = min(first + i * STEP, in.vocab - 1);
+        x[i] = logits[token];
+        y[i] = drafts[token];
+    }
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) {
+        const double p = weight((float)x[i], stop.most, in.scale) * of_p, q = weight((float)y[i], stop.draft_most, in.scale) * of_q;
+        w[i] = first + i * STEP < in.vocab ? fmax(p - q, 0.0) : 0.0;
+    }
 }
 template <class T>
 __device__ inline const T* draft_row(const VerifyIn& in, long long s, int i) {
@@ -448,11 +504,10 @@ __global__ __launch_bounds__(kSumThreads) void left_sums_kernel(VerifyIn in) {
     if (stop.row < 0 || !stop.drafted || !(stop.total > 0.0)) return;
     const T* x = (const T*)in.logits + (s * in.m + stop.row) * in.stride;
     const T* y = draft_row<T>(in, s, stop.row);
-    double sum = 0.0;
-    for (int i = 0; i < kLaneValues; ++i) {
-        const int token = block * kBlock + i * 64 + lane;
-        if (token < in.vocab) sum += left_of(stop, x, y, token, in.scale);
-    }
+    double w[kLaneValues], sum = 0.0;
+    left_weights<64>(stop, x, y, block * kBlock + lane, in, w);
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) sum += w[i];
     sum = wave_sum(sum);
     if (lane == 0) in.left[s * in.left_blocks + block] = sum;
 }
@@ -474,23 +529,12 @@ __global__ __launch_bounds__(64) void draw_left_kernel(VerifyIn in) {
     float logit = 0.f;
     if (stop.drafted && norm.total > 0.0) {
         const double* left = in.left + s * in.left_blocks;
-        double before, all;
-        const int block = pick_block(in.left_blocks, u, lane, before, [&](int b) { return left[b]; }, all);
-        if (block >= 0) {
+        const Picked picked = pick_block(in.left_blocks, u, lane, [&](int b) { return left[b]; });
+        if (picked.block >= 0) {
             const T* x = (const T*)in.logits + flat * in.stride;
-            const T* y = draft_row<T>(in, s, stop.row);
-            double base = before;
-            int last = -1;
-            for (int i = 0; i < kLaneValues && token < 0; ++i) {
-                const int v = block * kBlock + i * 64 + lane;
-                const double mine = v < in.vocab ? left_of(stop, x, y, v, in.scale) : 0.0;
-                const double upto = base + wave_scan(mine);
-                const uint64_t over = __ballot(mine > 0.0 && upto > u * all), some = __ballot(mine > 0.0);
-                if (over) token = block * kBlock + i * 64 + __ffsll((unsigned long long)over) - 1;
-                if (some) last = block * kBlock + i * 64 + 63 - __clzll((long long)some);
-                base = __shfl(upto, 63);
-            }
-            if (token < 0) token = last;
+            double w[kLaneValues];
+            left_weights<1>(stop, x, draft_row<T>(in, s, stop.row), picked.block * kBlock + lane * kLaneValues, in, w);
+            token = pick_token(w, picked.block * kBlock + lane * kLaneValues, picked);
             if (token >= 0) logit = (float)x[token];
         }
     }
@@ -507,8 +551,8 @@ int row_blocks(int32_t vocab) { return (int)(((int64_t)vocab + 7 + kBlock - 1) /
 int left_blocks(int32_t vocab) { return (int)(((int64_t)vocab + kBlock - 1) / kBlock); }
 
 struct VerifySpace {
-    size_t blocks, left, stops;
-    size_t bytes() const { return blocks + left + stops; }
+    size_t blocks, left, stops, said;
+    size_t bytes() const { return blocks + left + stops + said; }
 };
 VerifySpace verify_space(int64_t n, int32_t m, int32_t vocab, bool drafts) {
     VerifySpace v{};
@@ -516,6 +560,8 @@ VerifySpace verify_space(int64_t n, int32_t m, int32_t vocab, bool drafts) {
     if (drafts) {
         v.left = align_up((size_t)n * left_blocks(vocab) * sizeof(double));
         v.stops = align_up((size_t)n * sizeof(Stop));
+    } else {
+        v.said = align_up((size_t)(n * m) * sizeof(Said));
     }
     return v;
 }
@@ -534,7 +580,9 @@ int launch_verify(const VerifyIn& in, hipStream_t stream) {
     hipLaunchKernelGGL((block_sums_kernel<T>), dim3((unsigned)((rows * in.row_blocks + kWaves - 1) / kWaves)), dim3(kSumThreads), 0, stream, in);
     HIP_TRY(hipGetLastError());
     if (!in.drafts) {
-        hipLaunchKernelGGL((verify_tree_kernel<T>), dim3((unsigned)in.n), dim3(kWalkThreads), 0, stream, in);
+        hipLaunchKernelGGL((draw_rows_kernel<T>), dim3((unsigned)(in.n * in.m)), dim3(64), 0, stream, in);
+        HIP_TRY(hipGetLastError());
+        hipLaunchKernelGGL(verify_tree_kernel, dim3((unsigned)in.n), dim3(64), 0, stream, in);
         HIP_TRY(hipGetLastError());
         return IVFPQ_OK;
     }
@@ -581,7 +629,7 @@ int ivfpq_verify_drafts(const void* d_logits, int32_t dtype, int64_t n, int32_t 
         if (workspace_bytes < space.bytes()) return fail(IVFPQ_ENOSPACE, "%s: workspace %zu bytes, need %zu", what, workspace_bytes, space.bytes());
         char* ws = (char*)d_workspace;
         const VerifyIn in{d_logits, drafts ? d_draft_logits : nullptr, row_stride, draft_stride, d_tokens, d_parents, d_counts, d_uniforms, d_accept,
-                          (BlockSum*)ws, (double*)(ws + space.blocks), (Stop*)(ws + space.blocks + space.left), d_path, d_kept, d_next, d_logprobs, n, m, vocab,
+                          (BlockSum*)ws, (double*)(ws + space.blocks), (Stop*)(ws + space.blocks + space.left), (Said*)(ws + space.blocks + space.left + space.stops), d_path, d_kept, d_next, d_logprobs, n, m, vocab,
                           row_blocks(vocab), left_blocks(vocab), 1.4426950408889634 / temperature};
         return with_value_type(dtype, [&](auto t) { return launch_verify<decltype(t)>(in, (hipStream_t)hip_stream); });
     });
