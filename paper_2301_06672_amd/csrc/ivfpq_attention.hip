@@ -132,7 +132,7 @@ struct Columns {
     // Many columns' queries and sums stay in the registers that matrix instructions take and give their operands in.  Left to itself the compiler
     // moves all sums to others and back once a tile, since they are scaled there now and then.
     __device__ inline void settle() {
-        if constexpr (NQ * KC >= 8) {
+        if constexpr (NQ * KC >= 16) {
 #pragma unroll
             for (int t = 0; t < NQ; ++t) {
 #pragma unroll
@@ -235,7 +235,12 @@ struct Columns {
         float most[NQ];
 #pragma unroll
         for (int t = 0; t < NQ; ++t) {
-            most[t] = scale * max3(max3(score[t][0][0], score[t][0][1], score[t][0][2]), max3(score[t][0][3], score[t][1][0], score[t][1][1]), fmaxf(score[t][1][2], score[t][1][3]));
+            // NaN if a score is: the column is NaN then, whatever its reference.  (No inline assembly here: results of matrix instructions have to be waited
+            // for, which the compiler does for instructions that it knows.)
+            float x = score[t][0][0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) x = __builtin_elementwise_maximum(x, score[t][j >> 2][j & 3]);
+            most[t] = scale * x;
             ahead |= most[t] > reference[t] + kAhead;
         }
         if (__any(ahead)) {
@@ -469,43 +474,44 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_shared_kernel(Att
 // Many columns: each wave has its own and goes over all tiles, which pass through the LDS.  A tile is 4 KC operands of a wave, 1 KB each in the order of
 // the lanes, so that they come and go in whole lines: 2 KC of keys, then 2 KC of values.  A wave brings KC of them: into registers three tiles
 // ahead, into the LDS one tile ahead.
-template <class T, int KC, int NQ, bool EXACT>
-__global__ __launch_bounds__(kAttentionThreads) void attention_tiles_kernel(AttentionIn in) {
-    constexpr int VT = KC * 2, PARTS = 4 * KC;
+template <class T, int KC, int NQ, int WAVES, bool EXACT>
+__global__ __launch_bounds__(64 * WAVES) void attention_tiles_kernel(AttentionIn in) {
+    constexpr int VT = KC * 2, PARTS = 4 * KC, MINE = PARTS / WAVES;
     __shared__ u32x4 stage[2][PARTS][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, group = lane >> 4;
     const int d = EXACT ? KC * 32 : in.at.d;
-    const Piece p = piece_of(in, NQ * 64, 1);
+    const Piece p = piece_of(in, NQ * 16 * WAVES, 1);
     if (p.nothing) return;
     const int end = p.end, len = p.len;
-    const int first_col = (p.block * 4 + wave) * NQ * 16;
+    const int first_col = (p.block * WAVES + wave) * NQ * 16;
     Columns<T, KC, NQ, EXACT> cols;
     cols.start(in, p.s, p.head, first_col, p.count, in.parents ? tree_line(in, p.s, p.count, lane) : 0, d, lane);
 
     const int* pages = in.at.pages + p.s * in.at.stride;
     const long long page_values = in.at.page_values();
     const int in_page = in.at.page() - 1;
-    const bool for_values = wave >= 2;
+    const bool for_values = wave >= WAVES / 2;
+    const int part = wave * MINE % (2 * KC);         // of the keys' or the values' operands
     const bool second = for_values ? group >> 1 : col >> 3;         // in the tile's second 16 places
-    const int from_lane = for_values ? (group & 1) * 8 * d + col * 8 + (wave - 2) * KC * 128 : (key_place(lane) & 15) * d + group * 8 + wave * 4 * d;
+    const int from_lane = for_values ? (group & 1) * 8 * d + col * 8 + part * 128 : (key_place(lane) & 15) * d + group * 8 + part / KC * 4 * d + part % KC * 32;
     const T* const from_head = (const T*)(for_values ? in.v_cache : in.k_cache) + ((long long)p.head << in.at.shift) * d + from_lane;
     const int apart = for_values ? 128 : 32;
     struct Parts {
-        u32x4 of[KC];
+        u32x4 of[MINE];
     };
     const auto bring = [&](int tile, const TilePages& at, Parts& to) {
         const int off0 = (tile * kTile) & in_page, off1 = (tile * kTile + 16) & in_page;
         const T* from = from_head + (second ? max(at.second, 0) * page_values + off1 * d : max(at.first, 0) * page_values + off0 * d);
 #pragma unroll
-        for (int i = 0; i < KC; ++i) {
-            const bool some = EXACT || (for_values ? ((wave - 2) * KC + i) * 16 + col < d : i * 32 + group * 8 < d);
+        for (int i = 0; i < MINE; ++i) {             // MINE divides KC: keys of one half
+            const bool some = EXACT || (for_values ? (part + i) * 16 + col < d : (part % KC + i) * 32 + group * 8 < d);
             to.of[i] = some ? *reinterpret_cast<const u32x4*>(from + i * apart) : u32x4{};
         }
     };
     const auto put = [&](int tile, const Parts& parts) {
 #pragma unroll
-        for (int i = 0; i < KC; ++i) stage[tile & 1][wave * KC + i][lane] = parts.of[i];
+        for (int i = 0; i < MINE; ++i) stage[tile & 1][wave * MINE + i][lane] = parts.of[i];
     };
     int tile = p.first;
     TilePages now = tile_pages(in.at, pages, tile, end), next = tile_pages(in.at, pages, tile + 1, end), third = tile_pages(in.at, pages, tile + 2, end);
@@ -582,10 +588,12 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionIn in, lon
 template <class T, int KC, bool EXACT>
 int launch_attention(const AttentionIn& in, const AttentionPlan& plan, hipStream_t stream) {
     const long long passes = in.n * in.at.kv_heads * in.splits;
-    const dim3 grid((unsigned)((passes + 7) / 8 * 8 * in.blocks)), threads(kAttentionThreads);
+    const dim3 grid((unsigned)((passes + 7) / 8 * 8 * in.blocks)), threads(64 * plan.waves);
     constexpr int MOST = KC > 4 ? 2 : 4;             // tiles of columns whose sums fit a wave's registers
-    if (plan.apart && plan.tiles == 2) hipLaunchKernelGGL((attention_tiles_kernel<T, KC, 2, EXACT>), grid, threads, 0, stream, in);
-    else if (plan.apart) hipLaunchKernelGGL((attention_tiles_kernel<T, KC, MOST, EXACT>), grid, threads, 0, stream, in);
+    if (plan.apart && plan.waves == 4) hipLaunchKernelGGL((attention_tiles_kernel<T, KC, 2, 4, EXACT>), grid, threads, 0, stream, in);
+    else if (plan.apart) {
+        if constexpr (KC <= 4) hipLaunchKernelGGL((attention_tiles_kernel<T, KC, 2, 8, EXACT>), grid, threads, 0, stream, in);
+    }
     else if (plan.tiles == 1) hipLaunchKernelGGL((attention_shared_kernel<T, KC, 1, EXACT>), grid, threads, 0, stream, in);
     else if (plan.tiles == 2) hipLaunchKernelGGL((attention_shared_kernel<T, KC, 2, EXACT>), grid, threads, 0, stream, in);
     else if constexpr (MOST == 4) hipLaunchKernelGGL((attention_shared_kernel<T, KC, 4, EXACT>), grid, threads, 0, stream, in);

@@ -11,7 +11,8 @@ struct AttentionPlan {
     bool apart;                       // each wave has columns of its own; else the waves share them and divide the places
     int blocks;                       // of columns
     int splits;                       // of the places
-    int columns() const { return tiles * 16 * (apart ? 4 : 1); }
+    int waves;                        // of a workgroup
+    int columns() const { return tiles * 16 * (apart ? waves : 1); }
 };
 
 constexpr int kMostSplits = 64;
@@ -21,7 +22,8 @@ inline AttentionPlan attention_plan(int64_t n, int m, int heads, int kv_heads, i
     const int most = d > 128 ? 2 : 4;                               // tiles whose sums fit a wave's registers
     AttentionPlan p{};
     p.apart = columns > 16 * most;
-    p.tiles = p.apart ? (columns <= 128 ? 2 : most) : columns <= 16 ? 1 : columns <= 32 ? 2 : most;
+    p.tiles = p.apart ? 2 : columns <= 16 ? 1 : columns <= 32 ? 2 : most;
+    p.waves = p.apart && columns > 128 && d <= 128 ? 8 : 4;
     p.blocks = (int)((columns + p.columns() - 1) / p.columns());
     // workgroups for every CU twice over, each of at least two tiles of places a wave
     const int64_t groups = n * kv_heads * p.blocks;
