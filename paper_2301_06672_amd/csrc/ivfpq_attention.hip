@@ -92,10 +92,14 @@ struct TilePages {
     __device__ inline bool both() const { return first >= 0 && second >= 0; }
 };
 __device__ inline TilePages tile_pages(const Pages& at, const int* pages, int tile, int end) {
-    const long long place = (long long)tile * kTile, i0 = place >> at.shift, i1 = (place + 16) >> at.shift;
-    TilePages p{tile < end && i0 < at.most ? pages[i0] : -1, tile < end && i1 < at.most ? pages[i1] : -1};
-    if (p.first >= at.n_pages) p.first = -1;
-    if (p.second >= at.n_pages) p.second = -1;
+    // the table is read by scalar loads: nothing writes it while the kernel runs, and pages are the same for the whole wave
+    typedef const int __attribute__((address_space(4)))* table_t;
+    const table_t table = (table_t)(uintptr_t)pages;
+    const int n_pages = (int)at.n_pages;
+    const int i0 = (int)((unsigned)tile * kTile >> at.shift), i1 = (int)(((unsigned)tile * kTile + 16) >> at.shift);      // places are under 2^31
+    TilePages p{tile < end && i0 < at.most ? table[i0] : -1, tile < end && i1 < at.most ? table[i1] : -1};
+    if (p.first >= n_pages) p.first = -1;
+    if (p.second >= n_pages) p.second = -1;
     return p;
 }
 
@@ -471,17 +475,18 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_shared_kernel(Att
     if (wave == 0) cols.write(in, p.s, p.head, p.split, p.block * NQ * 16, d, lane);
 }
 
-// Many columns: each wave has its own and goes over all tiles, which pass through the LDS.  A tile is 4 KC operands of a wave, 1 KB each in the order of
-// the lanes, so that they come and go in whole lines: 2 KC of keys, then 2 KC of values.  A wave brings KC of them: into registers three tiles
-// ahead, into the LDS one tile ahead.
+// Many columns: each wave has its own and goes over all tiles, which pass through the LDS, `AT_ONCE` at a time (what is done once for two is a third of
+// the instructions for one).  A tile is 4 KC operands of a wave, 1 KB each in the order of the lanes, so that they come and go in whole
+// lines: 2 KC of keys, then 2 KC of values.  A wave brings MINE of them: from the cache into registers three steps before they are used, into the LDS two steps
+// before; the next tile's keys are read from there while this one's scores become weights.
 template <class T, int KC, int NQ, int WAVES, bool EXACT>
 __global__ __launch_bounds__(64 * WAVES) void attention_tiles_kernel(AttentionIn in) {
-    constexpr int VT = KC * 2, PARTS = 4 * KC, MINE = PARTS / WAVES;
-    __shared__ u32x4 stage[2][PARTS][64];
+    constexpr int VT = KC * 2, PARTS = 4 * KC, MINE = PARTS / WAVES, AT_ONCE = KC <= 4 ? 2 : 1;
+    __shared__ u32x4 stage[3][AT_ONCE][PARTS][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, group = lane >> 4;
     const int d = EXACT ? KC * 32 : in.at.d;
-    const Piece p = piece_of(in, NQ * 16 * WAVES, 1);
+    const Piece p = piece_of(in, NQ * 16 * WAVES, AT_ONCE);
     if (p.nothing) return;
     const int end = p.end, len = p.len;
     const int first_col = (p.block * WAVES + wave) * NQ * 16;
@@ -497,58 +502,90 @@ __global__ __launch_bounds__(64 * WAVES) void attention_tiles_kernel(AttentionIn
     const int from_lane = for_values ? (group & 1) * 8 * d + col * 8 + part * 128 : (key_place(lane) & 15) * d + group * 8 + part / KC * 4 * d + part % KC * 32;
     const T* const from_head = (const T*)(for_values ? in.v_cache : in.k_cache) + ((long long)p.head << in.at.shift) * d + from_lane;
     const int apart = for_values ? 128 : 32;
-    struct Parts {
-        u32x4 of[MINE];
-    };
-    const auto bring = [&](int tile, const TilePages& at, Parts& to) {
-        const int off0 = (tile * kTile) & in_page, off1 = (tile * kTile + 16) & in_page;
-        const T* from = from_head + (second ? max(at.second, 0) * page_values + off1 * d : max(at.first, 0) * page_values + off0 * d);
-#pragma unroll
-        for (int i = 0; i < MINE; ++i) {             // MINE divides KC: keys of one half
-            const bool some = EXACT || (for_values ? (part + i) * 16 + col < d : (part % KC + i) * 32 + group * 8 < d);
-            to.of[i] = some ? *reinterpret_cast<const u32x4*>(from + i * apart) : u32x4{};
+    struct StepPages {
+        TilePages of[AT_ONCE];
+        __device__ inline bool all() const {
+            bool every = true;
+            for (int u = 0; u < AT_ONCE; ++u) every = every && of[u].both();
+            return every;
         }
     };
-    const auto put = [&](int tile, const Parts& parts) {
+    const auto find = [&](int tile) {
+        StepPages to;
 #pragma unroll
-        for (int i = 0; i < MINE; ++i) stage[tile & 1][wave * MINE + i][lane] = parts.of[i];
+        for (int u = 0; u < AT_ONCE; ++u) to.of[u] = tile_pages(in.at, pages, tile + u, end);
+        return to;
     };
-    int tile = p.first;
-    TilePages now = tile_pages(in.at, pages, tile, end), next = tile_pages(in.at, pages, tile + 1, end), third = tile_pages(in.at, pages, tile + 2, end);
-    Parts ahead;                                     // the next tile's
+    u32x4 ahead[AT_ONCE][MINE];                      // the wave's operands of a step
+    const auto bring = [&](int tile, const StepPages& at) {         // (a tile behind the last is read as page 0)
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int off0 = ((tile + u) * kTile) & in_page, off1 = ((tile + u) * kTile + 16) & in_page;
+            const T* from = from_head + (second ? max(at.of[u].second, 0) * page_values + off1 * d : max(at.of[u].first, 0) * page_values + off0 * d);
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) {         // MINE divides KC: keys of one half
+                const bool some = EXACT || (for_values ? (part + i) * 16 + col < d : (part % KC + i) * 32 + group * 8 < d);
+                ahead[u][i] = some ? *reinterpret_cast<const u32x4*>(from + i * apart) : u32x4{};
+            }
+        }
+    };
+    const auto put = [&](int to) {
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) stage[to][u][wave * MINE + i][lane] = ahead[u][i];
+    };
+    u32x4 keys[2][KC], values[VT];
+    const auto read_keys = [&](const u32x4 (*from)[64]) {
+#pragma unroll
+        for (int i = 0; i < 2 * KC; ++i) keys[i / KC][i % KC] = from[i][lane];
+    };
+    int tile = p.first, at = 0;                      // the stage that this step is in
+    StepPages now = find(tile), next = find(tile + AT_ONCE), third = find(tile + 2 * AT_ONCE), fourth = find(tile + 3 * AT_ONCE);
     if (tile < end) {
-        bring(tile, now, ahead);
-        put(tile, ahead);
+        bring(tile, now);
+        put(0);
+        if (tile + AT_ONCE < end) {
+            bring(tile + AT_ONCE, next);
+            put(1);
+        }
+        if (tile + 2 * AT_ONCE < end) bring(tile + 2 * AT_ONCE, third);
+        __syncthreads();
+        read_keys(stage[0][0]);
     }
-    if (tile + 1 < end) bring(tile + 1, next, ahead);
     bool odd = false;
     const auto go = [&](auto masked) {
         constexpr bool MASKED = decltype(masked)::value;
-        __syncthreads();                             // this tile is there, and the other stage is free
-        const u32x4(*at)[64] = stage[tile & 1];
-        u32x4 keys[2][KC], values[VT];
-        cols.settle();
+        const int at1 = at == 2 ? 0 : at + 1, at2 = at1 == 2 ? 0 : at1 + 1;
+        __syncthreads();                             // the next step's tiles are there, and the stage of the one before is free
+        if (tile + 2 * AT_ONCE < end) put(at2);
+        if (tile + 3 * AT_ONCE < end) bring(tile + 3 * AT_ONCE, fourth);
+        const StepPages after = find(tile + 4 * AT_ONCE);
 #pragma unroll
-        for (int i = 0; i < 2 * KC; ++i) keys[i / KC][i % KC] = at[i][lane];
-        const TilePages after = tile_pages(in.at, pages, tile + 3, end);
-        if (tile + 1 < end) put(tile + 1, ahead);
-        if (tile + 2 < end) bring(tile + 2, third, ahead);
-        f32x4 score[NQ][2];
-        cols.scores(keys, score);
+        for (int u = 0; u < AT_ONCE; ++u) {
+            if (MASKED && tile + u >= end) break;
+            f32x4 score[NQ][2];
+            cols.settle();
 #pragma unroll
-        for (int i = 0; i < VT; ++i) values[i] = at[2 * KC + i][lane];
-        if constexpr (MASKED) {
-            const int first_place = tile * kTile + group * 8;
-            const bool there = group >> 1 ? now.second >= 0 : now.first >= 0;
-            cols.mask(in, score, first_place, len, there);
-            odd |= cols.tame(values, held_fields(there, first_place, p.places));
+            for (int i = 0; i < VT; ++i) values[i] = stage[at][u][2 * KC + i][lane];
+            cols.scores(keys, score);
+            __builtin_amdgcn_sched_barrier(0);
+            read_keys(u + 1 < AT_ONCE ? stage[at][u + 1 < AT_ONCE ? u + 1 : 0] : stage[at1][0]);      // (behind the last tile: of no meaning)
+            if constexpr (MASKED) {
+                const int first_place = (tile + u) * kTile + group * 8;
+                const bool there = group >> 1 ? now.of[u].second >= 0 : now.of[u].first >= 0;
+                cols.mask(in, score, first_place, len, there);
+                odd |= cols.tame(values, held_fields(there, first_place, p.places));
+            }
+            cols.weigh_and_add(score, in.scale, values);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        cols.weigh_and_add(score, in.scale, values);
-        now = next, next = third, third = after;
-        ++tile;
+        now = next, next = third, third = fourth, fourth = after;
+        tile += AT_ONCE;
+        at = at1;
     };
     const int seen_by_all = min(end, len / kTile);
-    while (tile < seen_by_all && now.both()) go(std::false_type{});
+    while (tile + AT_ONCE <= seen_by_all && now.all()) go(std::false_type{});
     const int first_masked = tile;
     while (tile < end) go(std::true_type{});
     if (__any(odd)) cols.add_odd(in, p.s, p.head, first_col, first_masked, end, 1, len, d, lane);
