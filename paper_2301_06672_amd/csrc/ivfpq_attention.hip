@@ -328,6 +328,7 @@ struct Piece {
     long long s;
     int head, split, block, len, count, first, end;
     long long places;                                // up to the last that one of the columns sees
+    int seen_by_all;                                 // tiles whose places every used column sees, if their pages are there
     bool nothing;                                    // no such piece
 };
 // cols: of a block; STEP: tiles that a part's number of tiles is a multiple of.
@@ -351,6 +352,8 @@ __device__ inline Piece piece_of(const AttentionIn& in, int cols, int step) {
     each = (each + step - 1) / step * step;
     p.first = (int)min((long long)p.split * each, (long long)tiles);
     p.end = min(p.first + each, tiles);
+    // of a chain's rows those up to the block's first
+    p.seen_by_all = min((int)(((long long)p.len + (in.parents ? 0 : p.block * cols / share + 1)) / kTile), p.end);
     return p;
 }
 
@@ -430,8 +433,7 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_shared_kernel(Att
         tile += STEP;
     };
     // tiles of places that every column sees, then those with rows, or (seldom) all from the first that lacks a page
-    const int seen_by_all = min(end, len / kTile);
-    while (tile < seen_by_all && now.both()) go(std::false_type{});
+    while (tile < p.seen_by_all && now.both()) go(std::false_type{});
     const int first_masked = tile;
     while (tile < end) go(std::true_type{});
     if (__any(odd)) cols.add_odd(in, p.s, p.head, p.block * NQ * 16, first_masked, end, STEP, len, d, lane);
@@ -584,8 +586,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_tiles_kernel(AttentionIn
         tile += AT_ONCE;
         at = at1;
     };
-    const int seen_by_all = min(end, len / kTile);
-    while (tile + AT_ONCE <= seen_by_all && now.all()) go(std::false_type{});
+    while (tile + AT_ONCE <= p.seen_by_all && now.all()) go(std::false_type{});
     const int first_masked = tile;
     while (tile < end) go(std::true_type{});
     if (__any(odd)) cols.add_odd(in, p.s, p.head, first_col, first_masked, end, 1, len, d, lane);
