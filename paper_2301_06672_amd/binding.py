@@ -152,7 +152,8 @@ def _hp(a: np.ndarray):
 
 
 def _dp(t: Optional[torch.Tensor]):
-    return ctypes.c_void_p(t.data_ptr()) if t is not None else None
+    # an int, which ctypes takes for a pointer by the declared types; an object for it would take as long as the conversion of ten
+    return t.data_ptr() if t is not None else None
 
 
 def _stream():

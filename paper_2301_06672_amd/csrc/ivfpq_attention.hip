@@ -46,11 +46,12 @@ struct AttentionIn {
     const void *q, *k_cache, *v_cache;
     void* out;
     float* lse;                       // [n * m][heads] or null
-    float* sums;                      // splits > 1: [n * m * heads][splits][d]
-    float2* norms;                    // [n * m * heads][splits]: reference, sum of weights
+    float* sums;                      // parts > 0: [kv_heads][blocks][parts + n][cols][d], of part p's share of sequence s in place p + s
+    float2* norms;                    // [kv_heads][blocks][parts + n][cols]: reference, sum of weights
+    int2* spans;                      // [n][blocks]: the first and the last part that have a share of the sequence
     const int* parents;               // [n][m] or null
     long long q_stride, out_stride, n;
-    int heads, blocks, splits;
+    int heads, blocks, parts, cols;
     float scale;                      // its size, with log2(e): not 0, so that -inf stays what it is
     bool negative;
     Pages at;
@@ -289,7 +290,8 @@ struct Columns {
         }
     }
 
-    __device__ inline void write(const AttentionIn& in, long long s, int head, int split, int first_col, int d, int lane) const {
+    // piece: where the sums of a part of the places go, -1: these are all.
+    __device__ inline void write(const AttentionIn& in, long long s, int head, int block, long long piece, int first_col, int d, int lane) const {
         const int share = in.heads / in.at.kv_heads, col = lane & 15, group = lane >> 4;
 #pragma unroll
         for (int t = 0; t < NQ; ++t) {
@@ -297,8 +299,8 @@ struct Columns {
             if (x >= in.at.m * share) continue;
             const int h = head * share + x % share;
             const long long flat = s * in.at.m + x / share;
-            if (in.splits > 1) {
-                const long long at = (flat * in.heads + h) * in.splits + split;
+            if (piece >= 0) {
+                const long long at = piece * in.cols + (x - block * in.cols);
                 if (group == 0) in.norms[at] = make_float2(reference[t], total[t]);
 #pragma unroll
                 for (int v = 0; v < VT; ++v) {
@@ -323,37 +325,91 @@ struct Columns {
     }
 };
 
-// What a workgroup does: a block of columns of a head of a sequence over a part of the tiles of places.
+// What a workgroup does: a block of columns of a head of a sequence, over tiles of its places.
 struct Piece {
     long long s;
-    int head, split, block, len, count, first, end;
+    int head, block, len, count, first, end;
     long long places;                                // up to the last that one of the columns sees
     int seen_by_all;                                 // tiles whose places every used column sees, if their pages are there
+    long long slot;                                  // where its sums go; -1: they are all of the sequence's
     bool nothing;                                    // no such piece
 };
-// cols: of a block; STEP: tiles that a part's number of tiles is a multiple of.
-__device__ inline Piece piece_of(const AttentionIn& in, int cols, int step) {
+
+__device__ inline int tiles_of(const AttentionIn& in, int block, int len, int count, long long& places) {
+    const int share = in.heads / in.at.kv_heads, used = count * share, last_col = min((block + 1) * in.cols, used) - 1;
+    places = block * in.cols >= used ? 0 : in.parents ? (long long)len + count : (long long)len + last_col / share + 1;
+    return (int)min((places + kTile - 1) / kTile, (((long long)in.at.most << in.at.shift) + kTile - 1) / kTile);
+}
+
+// Without parts a piece is a whole sequence.  With them the tiles of all sequences lie behind each other (each has one at least, whose piece writes its rows
+// whatever it finds; fewer than 2^31 in all), a part is as many of these as any other but the last, and a piece is what a part has of a sequence:
+// part p's of sequence s is number p + s.
+__device__ inline Piece piece_of(const AttentionIn& in, int lane) {
     // blocks of columns that read the same places are 8 workgroups apart: on one XCD, whose L2 they share
-    const unsigned order = blockIdx.x, turn = order / 8;
+    const unsigned order = blockIdx.x, turn = order / 8, n = (unsigned)in.n, kv_heads = (unsigned)in.at.kv_heads;      // under 2^23 workgroups
+    const unsigned pass = turn / in.blocks * 8 + order % 8;
     Piece p{};
     p.block = (int)(turn % in.blocks);
-    const unsigned pass = turn / in.blocks * 8 + order % 8, n = (unsigned)in.n;      // (split, head, sequence); under 2^23 workgroups
-    p.nothing = pass >= n * (unsigned)(in.at.kv_heads * in.splits);
-    if (p.nothing) return p;
-    p.s = pass % n;
-    p.head = (int)(pass / n % in.at.kv_heads);
-    p.split = (int)(pass / n / in.at.kv_heads);
-    p.len = in.at.len(p.s);
-    p.count = in.at.count(p.s);
-    const int share = in.heads / in.at.kv_heads, used = p.count * share, last_col = min((p.block + 1) * cols, used) - 1;
-    p.places = p.block * cols >= used ? 0 : in.parents ? (long long)p.len + p.count : (long long)p.len + last_col / share + 1;
-    const int tiles = (int)min((p.places + kTile - 1) / kTile, (((long long)in.at.most << in.at.shift) + kTile - 1) / kTile);
-    int each = (tiles + in.splits - 1) / in.splits;
-    each = (each + step - 1) / step * step;
-    p.first = (int)min((long long)p.split * each, (long long)tiles);
-    p.end = min(p.first + each, tiles);
+    p.slot = -1;
+    unsigned part = 0, before = 0, each = 0;         // before: tiles of the sequences before this one; each: of a part
+    if (!in.parts) {
+        p.nothing = pass >= n * kv_heads;
+        if (p.nothing) return p;
+        p.s = pass % n;
+        p.head = (int)(pass / n);
+    } else {
+        p.nothing = pass >= kv_heads * (unsigned)(in.parts + in.n);
+        if (p.nothing) return p;
+        const unsigned number = pass / kv_heads;
+        p.head = (int)(pass - number * kv_heads);
+        const auto tiles = [&](unsigned s) {
+            long long places;
+            return s < n ? (unsigned)max(tiles_of(in, p.block, in.at.len(s), in.at.count(s), places), 1) : 0u;
+        };
+        unsigned all = n == 1 ? tiles(0) : 0;
+        if (n > 1) {
+            for (unsigned s = lane; s < n; s += 64) all += tiles(s);
+            for (int off = 32; off; off >>= 1) all += __shfl_xor(all, off);
+        }
+        all = __builtin_amdgcn_readfirstlane(all);
+        each = (all + in.parts - 1) / in.parts;
+        if (n == 1) p.nothing = number * each >= all;
+        uint64_t found = n == 1;
+        for (unsigned base = 0; base < n && !found; base += 64) {
+            const unsigned mine = tiles(base + lane);
+            unsigned upto = mine;
+            for (int off = 1; off < 64; off <<= 1) {
+                const unsigned below = __shfl_up(upto, off);
+                if (lane >= off) upto += below;
+            }
+            const unsigned of = number - (base + lane), from = before + upto - mine;      // of: the part, if it has a share of the lane's sequence
+            found = __ballot(mine > 0 && number >= base + lane && of < (unsigned)in.parts && max(of * each, from) < min((of + 1) * each, before + upto));
+            if (found) {
+                const int l = __ffsll((unsigned long long)found) - 1;
+                p.s = __builtin_amdgcn_readfirstlane(base + l);
+                before = __shfl(from, l);
+            } else before += __shfl(upto, 63);
+        }
+        p.nothing = p.nothing || !found;
+        if (p.nothing) return p;
+        part = number - (unsigned)p.s;
+        before = __builtin_amdgcn_readfirstlane(before);
+    }
+    p.len = __builtin_amdgcn_readfirstlane(in.at.len(p.s));
+    p.count = __builtin_amdgcn_readfirstlane(in.at.count(p.s));
+    const int tiles = tiles_of(in, p.block, p.len, p.count, p.places);
+    p.end = tiles;
+    if (in.parts) {
+        const unsigned start = part * each;
+        p.first = start > before ? min((int)(start - before), tiles) : 0;
+        p.end = (int)min(start + each - before, (unsigned)tiles);
+        // the parts that the sequence's first and last tile are in
+        const unsigned first = before / each, last = (before + max(tiles, 1) - 1) / each;
+        if (first != last) p.slot = ((long long)p.head * in.blocks + p.block) * (in.parts + in.n) + part + p.s;
+        if (part == first && p.head == 0 && threadIdx.x == 0) in.spans[p.s * in.blocks + p.block] = make_int2((int)first, (int)last);
+    }
     // of a chain's rows those up to the block's first
-    p.seen_by_all = min((int)(((long long)p.len + (in.parents ? 0 : p.block * cols / share + 1)) / kTile), p.end);
+    p.seen_by_all = min((int)(((long long)p.len + (in.parents ? 0 : p.block * in.cols / (in.heads / in.at.kv_heads) + 1)) / kTile), p.end);
     return p;
 }
 
@@ -377,7 +433,9 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_shared_kernel(Att
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, group = lane >> 4;
     const int d = EXACT ? KC * 32 : in.at.d;
-    const Piece p = piece_of(in, NQ * 16, STEP);
+    __shared__ float refs[4][NQ][16], totals[4][NQ][16];
+    __shared__ f32x4 shared[2][NQ][VT][64];
+    const Piece p = piece_of(in, lane);
     if (p.nothing) return;
     const int end = p.end, len = p.len;
     Columns<T, KC, NQ, EXACT> cols;
@@ -440,8 +498,6 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_shared_kernel(Att
 
     cols.finish();
     // the waves' sums about the largest of their references, added up in a fixed order: 0 + 2, 1 + 3, then both
-    __shared__ float refs[4][NQ][16], totals[4][NQ][16];
-    __shared__ f32x4 shared[2][NQ][VT][64];
     if (group == 0)
 #pragma unroll
         for (int t = 0; t < NQ; ++t) {
@@ -474,7 +530,7 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_shared_kernel(Att
                 for (int v = 0; v < VT; ++v) cols.sums[t][v] += shared[wave][t][v][lane];
         __syncthreads();
     }
-    if (wave == 0) cols.write(in, p.s, p.head, p.split, p.block * NQ * 16, d, lane);
+    if (wave == 0) cols.write(in, p.s, p.head, p.block, p.slot, p.block * NQ * 16, d, lane);
 }
 
 // Many columns: each wave has its own and goes over all tiles, which pass through the LDS, `AT_ONCE` at a time (what is done once for two is a third of
@@ -488,7 +544,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_tiles_kernel(AttentionIn
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, group = lane >> 4;
     const int d = EXACT ? KC * 32 : in.at.d;
-    const Piece p = piece_of(in, NQ * 16 * WAVES, AT_ONCE);
+    const Piece p = piece_of(in, lane);
     if (p.nothing) return;
     const int end = p.end, len = p.len;
     const int first_col = (p.block * WAVES + wave) * NQ * 16;
@@ -571,7 +627,6 @@ __global__ __launch_bounds__(64 * WAVES) void attention_tiles_kernel(AttentionIn
 #pragma unroll
             for (int i = 0; i < VT; ++i) values[i] = stage[at][u][2 * KC + i][lane];
             cols.scores(keys, score);
-            __builtin_amdgcn_sched_barrier(0);
             read_keys(u + 1 < AT_ONCE ? stage[at][u + 1 < AT_ONCE ? u + 1 : 0] : stage[at1][0]);      // (behind the last tile: of no meaning)
             if constexpr (MASKED) {
                 const int first_place = (tile + u) * kTile + group * 8;
@@ -580,7 +635,6 @@ __global__ __launch_bounds__(64 * WAVES) void attention_tiles_kernel(AttentionIn
                 odd |= cols.tame(values, held_fields(there, first_place, p.places));
             }
             cols.weigh_and_add(score, in.scale, values);
-            __builtin_amdgcn_sched_barrier(0);
         }
         now = next, next = third, third = fourth, fourth = after;
         tile += AT_ONCE;
@@ -591,30 +645,35 @@ __global__ __launch_bounds__(64 * WAVES) void attention_tiles_kernel(AttentionIn
     while (tile < end) go(std::true_type{});
     if (__any(odd)) cols.add_odd(in, p.s, p.head, first_col, first_masked, end, 1, len, d, lane);
     cols.finish();
-    cols.write(in, p.s, p.head, p.split, first_col, d, lane);
+    cols.write(in, p.s, p.head, p.block, p.slot, first_col, d, lane);
 }
 
-// The parts of a row and head added up: a thread has 4 components of one of them.
+// The pieces of a row and head added up, in their order: a thread has 4 components.
 template <class T>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttentionIn in, long long pieces) {
+__global__ __launch_bounds__(256) void attention_join_kernel(AttentionIn in, long long threads) {
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= pieces) return;
-    const int d = in.at.d, per = d / 4;
-    const long long at = i / per;                    // row and head
-    const int c = (int)(i % per) * 4;
+    if (i >= threads) return;
+    const int d = in.at.d, per = d / 4, share = in.heads / in.at.kv_heads;
+    const long long at = i / per, row = at / in.heads, s = row / in.at.m;
+    const int c = (int)(i - at * per) * 4, h = (int)(at - row * in.heads), head = h / share;
+    const int x = (int)(row - s * in.at.m) * share + h % share, block = x / in.cols;
+    const int2 span = in.spans[s * in.blocks + block];
+    if (span.x == span.y) return;                    // in one piece, and written
+    const long long first = ((((long long)head * in.blocks + block) * (in.parts + in.n) + span.x + s) * in.cols) + x % in.cols;
+    const int pieces = span.y - span.x + 1;
     float most = -INFINITY;
-    for (int p = 0; p < in.splits; ++p) most = fmaxf(most, in.norms[at * in.splits + p].x);
+    for (int p = 0; p < pieces; ++p) most = fmaxf(most, in.norms[first + (long long)p * in.cols].x);
     f32x4 sum{};
     float total = 0.f;
-    for (int p = 0; p < in.splits; ++p) {
-        const float2 norm = in.norms[at * in.splits + p];
+#pragma unroll 4
+    for (int p = 0; p < pieces; ++p) {
+        const long long piece = first + (long long)p * in.cols;
+        const float2 norm = in.norms[piece];
         const float by = shrink_by(norm.x, most);
         total += norm.y * by;
-        sum += *reinterpret_cast<const f32x4*>(in.sums + (at * in.splits + p) * d + c) * by;
+        sum += *reinterpret_cast<const f32x4*>(in.sums + piece * d + c) * by;
     }
     const float by = total == 0.f ? 0.f : 1.f / total;
-    const long long row = at / in.heads;
-    const int h = (int)(at % in.heads);
     if (in.lse && c == 0) in.lse[at] = total == 0.f ? -INFINITY : (most + __log2f(total)) * kLn2;
     typedef T v4 __attribute__((ext_vector_type(4)));
     v4 y;
@@ -625,7 +684,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionIn in, lon
 
 template <class T, int KC, bool EXACT>
 int launch_attention(const AttentionIn& in, const AttentionPlan& plan, hipStream_t stream) {
-    const long long passes = in.n * in.at.kv_heads * in.splits;
+    const long long passes = in.at.kv_heads * (in.parts + in.n);
     const dim3 grid((unsigned)((passes + 7) / 8 * 8 * in.blocks)), threads(64 * plan.waves);
     constexpr int MOST = KC > 4 ? 2 : 4;             // tiles of columns whose sums fit a wave's registers
     if (plan.apart && plan.waves == 4) hipLaunchKernelGGL((attention_tiles_kernel<T, KC, 2, 4, EXACT>), grid, threads, 0, stream, in);
@@ -636,9 +695,9 @@ int launch_attention(const AttentionIn& in, const AttentionPlan& plan, hipStream
     else if (plan.tiles == 2) hipLaunchKernelGGL((attention_shared_kernel<T, KC, 2, EXACT>), grid, threads, 0, stream, in);
     else if constexpr (MOST == 4) hipLaunchKernelGGL((attention_shared_kernel<T, KC, 4, EXACT>), grid, threads, 0, stream, in);
     HIP_TRY(hipGetLastError());
-    if (in.splits > 1) {
-        const long long pieces = in.n * in.at.m * in.heads * (in.at.d / 4);
-        hipLaunchKernelGGL((attention_join_kernel<T>), dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, stream, in, pieces);
+    if (in.parts) {
+        const long long all = in.n * in.at.m * in.heads * (in.at.d / 4);       // few, or the places would not be divided
+        hipLaunchKernelGGL((attention_join_kernel<T>), dim3((unsigned)((all + 255) / 256)), dim3(256), 0, stream, in, all);
         HIP_TRY(hipGetLastError());
     }
     return IVFPQ_OK;
@@ -663,7 +722,7 @@ bool known_shape(int64_t n, int32_t m, int32_t heads, int32_t kv_heads, int32_t 
            n * m * heads <= ((int64_t)1 << 26);
 }
 // a launch has fewer than 2^32 threads
-bool fits_launch(int64_t n, int32_t kv_heads, const AttentionPlan& plan) { return n * kv_heads * plan.splits * plan.blocks <= ((int64_t)1 << 23); }
+bool fits_launch(int64_t n, int32_t kv_heads, const AttentionPlan& plan) { return (plan.parts + n) * kv_heads * plan.blocks <= ((int64_t)1 << 23); }
 
 }  // namespace
 
@@ -672,7 +731,7 @@ extern "C" {
 size_t ivfpq_draft_attention_workspace_bytes(int64_t n, int32_t m, int32_t heads, int32_t kv_heads, int32_t d, int64_t max_places) {
     if (!known_shape(n, m, heads, kv_heads, d, max_places)) return 0;
     const AttentionPlan plan = attention_plan(n, m, heads, kv_heads, d, max_places);
-    return align_up((size_t)attention_split_floats(n, m, heads, d, plan.splits) * sizeof(float));
+    return align_up((size_t)attention_scratch_bytes(n, kv_heads, d, plan));
 }
 
 int ivfpq_draft_attention(const void* d_q, int64_t q_stride, int32_t heads, int64_t n, int32_t m, const int32_t* d_parents, const int32_t* d_counts,
@@ -695,15 +754,17 @@ int ivfpq_draft_attention(const void* d_q, int64_t q_stride, int32_t heads, int6
         if ((uintptr_t)d_q % 16 || (uintptr_t)d_out % 8 || (uintptr_t)d_lse % 4) return fail(IVFPQ_EINVAL, "%s: queries are not aligned to 16 bytes, or the output not to 8", what);
         const AttentionPlan plan = attention_plan(n, m, heads, kv_heads, d, max_places);
         if (!fits_launch(n, kv_heads, plan)) return fail(IVFPQ_EUNSUPPORTED, "%s: n=%lld m=%d heads=%d kv_heads=%d: over 2^23 workgroups", what, (long long)n, m, heads, kv_heads);
-        const size_t need = align_up((size_t)attention_split_floats(n, m, heads, d, plan.splits) * sizeof(float));
+        const size_t need = align_up((size_t)attention_scratch_bytes(n, kv_heads, d, plan));
         if (need) {
             if (!d_workspace) return fail(IVFPQ_EINVAL, "%s: null workspace", what);
             if ((uintptr_t)d_workspace % kAlign) return fail(IVFPQ_EINVAL, "%s: workspace not aligned to %zu bytes", what, kAlign);
             if (workspace_bytes < need) return fail(IVFPQ_ENOSPACE, "%s: workspace %zu bytes, need %zu", what, workspace_bytes, need);
         }
-        AttentionIn in{d_q, d_k_cache, d_v_cache, d_out, d_lse, (float*)d_workspace, nullptr, d_parents, q_stride, out_stride, n, heads, plan.blocks, plan.splits,
-                       (float)std::max(std::abs((double)scale) * 1.4426950408889634, 1e-37), scale < 0.f, pages_in(d_pages, max_pages, d_lens, d_counts, n_pages, kv_heads, page, d, m)};
-        in.norms = (float2*)(in.sums + (size_t)rows * heads * plan.splits * d);      // d is a multiple of 8
+        AttentionIn in{d_q, d_k_cache, d_v_cache, d_out, d_lse, (float*)d_workspace, nullptr, nullptr, d_parents, q_stride, out_stride, n, heads, plan.blocks, plan.parts, plan.columns(),
+                       (float)std::min(std::max(std::abs((double)scale) * 1.4426950408889634, 1e-37), 3e38), scale < 0.f, pages_in(d_pages, max_pages, d_lens, d_counts, n_pages, kv_heads, page, d, m)};
+        const size_t pieces = (size_t)attention_pieces(n, kv_heads, plan);
+        in.norms = (float2*)(in.sums + pieces * d);        // d is a multiple of 8
+        in.spans = (int2*)(in.norms + pieces);
         // max_places bounds what is looked at: the table's end does
         in.at.most = n_pages ? (int)std::min<int64_t>(max_pages, (max_places + page - 1) / page) : 0;
         return with_value_type(cache_dtype, [&](auto t) {

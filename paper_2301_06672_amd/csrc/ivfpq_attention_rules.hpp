@@ -9,13 +9,13 @@ namespace ivfpq {
 struct AttentionPlan {
     int tiles;                        // of 16 columns a wave; a column is a row of the pass for one of the heads that share keys
     bool apart;                       // each wave has columns of its own; else the waves share them and divide the places
-    int blocks;                       // of columns
-    int splits;                       // of the places
     int waves;                        // of a workgroup
+    int blocks;                       // of columns
+    int parts;                        // that the places of all sequences together are dealt to, for each head and block; 0: a workgroup a sequence
     int columns() const { return tiles * 16 * (apart ? waves : 1); }
 };
 
-constexpr int kMostSplits = 64;
+constexpr int kMostPartsEach = 64;    // of a sequence, on average: what is joined one after the other
 
 inline AttentionPlan attention_plan(int64_t n, int m, int heads, int kv_heads, int d, int64_t max_places) {
     const int64_t columns = (int64_t)m * (heads / kv_heads);
@@ -25,16 +25,22 @@ inline AttentionPlan attention_plan(int64_t n, int m, int heads, int kv_heads, i
     p.tiles = p.apart ? 2 : columns <= 16 ? 1 : columns <= 32 ? 2 : most;
     p.waves = p.apart && columns > 128 && d <= 128 ? 8 : 4;
     p.blocks = (int)((columns + p.columns() - 1) / p.columns());
-    // workgroups for every CU twice over, each of at least two tiles of places a wave
-    const int64_t groups = n * kv_heads * p.blocks;
-    const int64_t useful = max_places / (p.apart ? 128 : 256);
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(512 + groups - 1) / groups, useful, kMostSplits}));
+    // where sequences are too few to fill the GPU: parts for every CU twice over, of two tiles a wave at least.  They are equal whatever the lengths.
+    // The kernel of eight waves leaves room for one workgroup on a CU: a part for each of one sequence, and of several, whose pieces differ, two rounds
+    // of pieces (64 rows of 16 sequences of 2,111 to 8,191 places, 32 heads of 128 over 8: 384, 512, 640, 768, 1,024 pieces take 181, 161, 162, 170, 174 us,
+    // and joining them 13, 16, 18, 22, 28).
+    const int64_t groups = (int64_t)kv_heads * p.blocks, useful = n * max_places / (p.apart ? 128 : 256);
+    const int64_t wanted = p.waves == 8 ? (n == 1 ? (256 + groups - 1) / groups : 512 / groups - n) : (512 + groups - 1) / groups;
+    const int64_t parts = std::min<int64_t>({wanted, useful, kMostPartsEach * n});
+    p.parts = parts > n && n * (max_places / 32 + 2) < ((int64_t)1 << 31) ? (int)parts : 0;
     return p;
 }
 
-// scratch of split places: for every row, head and split the sums of d components, then the reference and the sum of weights
-inline int64_t attention_split_floats(int64_t n, int m, int heads, int d, int splits) {
-    return splits == 1 ? 0 : n * m * heads * splits * ((int64_t)d + 2);
+// Scratch of divided places, in bytes: for every head, block and piece (a part's share of a sequence) the sums of d components for each column, then their
+// references and sums of weights; then the first and last part of every sequence and block.
+inline int64_t attention_pieces(int64_t n, int kv_heads, const AttentionPlan& p) { return p.parts ? (int64_t)kv_heads * p.blocks * (p.parts + n) * p.columns() : 0; }
+inline int64_t attention_scratch_bytes(int64_t n, int kv_heads, int d, const AttentionPlan& p) {
+    return p.parts ? attention_pieces(n, kv_heads, p) * ((int64_t)d + 2) * 4 + n * p.blocks * 8 : 0;
 }
 
 }  // namespace ivfpq

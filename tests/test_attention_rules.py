@@ -9,9 +9,11 @@ SHIM = """
 #include "ivfpq_attention_rules.hpp"
 extern "C" void plan(long long n, int m, int heads, int kv_heads, int d, long long places, int* out) {
     const ivfpq::AttentionPlan p = ivfpq::attention_plan(n, m, heads, kv_heads, d, places);
-    out[0] = p.tiles, out[1] = p.apart, out[2] = p.blocks, out[3] = p.splits, out[4] = p.columns();
+    out[0] = p.tiles, out[1] = p.apart, out[2] = p.blocks, out[3] = p.parts, out[4] = p.columns(), out[5] = p.waves;
 }
-extern "C" long long floats(long long n, int m, int heads, int d, int splits) { return ivfpq::attention_split_floats(n, m, heads, d, splits); }
+extern "C" long long scratch(long long n, int m, int heads, int kv_heads, int d, long long places) {
+    return ivfpq::attention_scratch_bytes(n, kv_heads, d, ivfpq::attention_plan(n, m, heads, kv_heads, d, places));
+}
 """
 
 
@@ -23,14 +25,14 @@ def plan(tmp_path_factory):
     subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-I", csrc, str(where / "shim.cpp"), "-o", str(where / "shim.so")], check=True)
     lib = ctypes.CDLL(str(where / "shim.so"))
     lib.plan.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_longlong, ctypes.POINTER(ctypes.c_int)]
-    lib.floats.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int]
-    lib.floats.restype = ctypes.c_longlong
+    lib.scratch.argtypes = lib.plan.argtypes[:-1]
+    lib.scratch.restype = ctypes.c_longlong
 
     def ask(*args):
-        out = (ctypes.c_int * 5)()
+        out = (ctypes.c_int * 6)()
         lib.plan(*args, out)
-        return dict(zip(("tiles", "apart", "blocks", "splits", "columns"), out))
-    ask.floats = lib.floats
+        return dict(zip(("tiles", "apart", "blocks", "parts", "columns", "waves"), out))
+    ask.scratch = lib.scratch
     return ask
 
 
@@ -43,15 +45,17 @@ def test_every_column_has_a_place(plan, d, share, m):
             continue
         for places in (0, 1, 127, 4_096, 2 ** 31 - 2 ** 21):
             got = plan(n, m, share * kv_heads, kv_heads, d, places)
-            assert got["tiles"] in (1, 2, 4) and not (d > 128 and got["tiles"] == 4)
+            assert got["tiles"] in (1, 2, 4) and not (d > 128 and got["tiles"] == 4) and got["waves"] in (4, 8)
             assert got["columns"] * got["blocks"] >= m * share > got["columns"] * (got["blocks"] - 1)
-            assert 1 <= got["splits"] <= 64
+            assert got["parts"] == 0 or n < got["parts"] <= 64 * n
             # workgroups that share a wave's columns have one block of them: they divide the places, and add up in the LDS
             assert got["apart"] or got["blocks"] == 1
 
 
 def test_places_are_divided_where_workgroups_are_few(plan):
-    assert plan(1, 1, 32, 8, 128, 100)["splits"] == 1                    # too short
-    assert plan(1, 1, 32, 8, 128, 100_000)["splits"] > 8
-    assert plan(1_000, 1, 32, 8, 128, 100_000)["splits"] == 1            # workgroups enough
-    assert plan.floats(3, 5, 8, 64, 1) == 0 and plan.floats(3, 5, 8, 64, 4) == 3 * 5 * 8 * 4 * 66
+    assert plan(1, 1, 32, 8, 128, 100)["parts"] == 0                     # too short
+    assert plan(1, 1, 32, 8, 128, 100_000)["parts"] == 64
+    assert plan(16, 64, 32, 8, 128, 8_192)["parts"] == 48                # two rounds of pieces, 8 x (48 + 16)
+    assert plan(1_000, 1, 32, 8, 128, 100_000)["parts"] == 0             # workgroups enough
+    assert plan.scratch(1_000, 1, 32, 8, 128, 100_000) == 0
+    assert plan.scratch(16, 64, 32, 8, 128, 8_192) == 8 * (48 + 16) * 256 * 130 * 4 + 16 * 8
