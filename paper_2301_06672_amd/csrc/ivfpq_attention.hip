@@ -134,20 +134,6 @@ struct Columns {
         }
     }
 
-    // Many columns' queries and sums stay in the registers that matrix instructions take and give their operands in.  Left to itself the compiler
-    // moves all sums to others and back once a tile, since they are scaled there now and then.
-    __device__ inline void settle() {
-        if constexpr (NQ * KC >= 16) {
-#pragma unroll
-            for (int t = 0; t < NQ; ++t) {
-#pragma unroll
-                for (int c = 0; c < KC; ++c) asm volatile("" : "+a"(q[t][c]));
-#pragma unroll
-                for (int v = 0; v < VT; ++v) asm volatile("" : "+a"(sums[t][v]));
-            }
-        }
-    }
-
     // S of a tile: the product of its keys, whose rows are dealt as key_place says, and the queries
     __device__ inline void scores(const u32x4 (&keys)[2][KC], f32x4 (&score)[NQ][2]) const {
 #pragma unroll
@@ -261,7 +247,6 @@ struct Columns {
                 for (int v = 0; v < VT; ++v) sums[t][v] *= shrink;
             }
         }
-        settle();
 #pragma unroll
         for (int t = 0; t < NQ; ++t) {
             const float r = reference[t] == -INFINITY ? 0.f : reference[t];      // nothing seen so far
@@ -476,7 +461,6 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_shared_kernel(Att
         const TilePages after = tile_pages(in.at, pages, tile + 2 * STEP, end);
         const bool more = tile + STEP < end;
         f32x4 score[NQ][2];
-        cols.settle();
         cols.scores(keys, score);
         if (more) load_keys(tile + STEP, next);
         if constexpr (MASKED) {
@@ -539,7 +523,7 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_shared_kernel(Att
 // before; the next tile's keys are read from there while this one's scores become weights.
 template <class T, int KC, int NQ, int WAVES, bool EXACT>
 __global__ __launch_bounds__(64 * WAVES) void attention_tiles_kernel(AttentionIn in) {
-    constexpr int VT = KC * 2, PARTS = 4 * KC, MINE = PARTS / WAVES, AT_ONCE = KC <= 4 ? 2 : 1;
+    constexpr int VT = KC * 2, PARTS = 4 * KC, MINE = PARTS / WAVES, AT_ONCE = WAVES == 8 ? 2 : 1;
     __shared__ u32x4 stage[3][AT_ONCE][PARTS][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, group = lane >> 4;
@@ -623,7 +607,6 @@ __global__ __launch_bounds__(64 * WAVES) void attention_tiles_kernel(AttentionIn
         for (int u = 0; u < AT_ONCE; ++u) {
             if (MASKED && tile + u >= end) break;
             f32x4 score[NQ][2];
-            cols.settle();
 #pragma unroll
             for (int i = 0; i < VT; ++i) values[i] = stage[at][u][2 * KC + i][lane];
             cols.scores(keys, score);
@@ -686,14 +669,12 @@ template <class T, int KC, bool EXACT>
 int launch_attention(const AttentionIn& in, const AttentionPlan& plan, hipStream_t stream) {
     const long long passes = in.at.kv_heads * (in.parts + in.n);
     const dim3 grid((unsigned)((passes + 7) / 8 * 8 * in.blocks)), threads(64 * plan.waves);
-    constexpr int MOST = KC > 4 ? 2 : 4;             // tiles of columns whose sums fit a wave's registers
-    if (plan.apart && plan.waves == 4) hipLaunchKernelGGL((attention_tiles_kernel<T, KC, 2, 4, EXACT>), grid, threads, 0, stream, in);
-    else if (plan.apart) {
-        if constexpr (KC <= 4) hipLaunchKernelGGL((attention_tiles_kernel<T, KC, 2, 8, EXACT>), grid, threads, 0, stream, in);
+    if (!plan.apart && plan.tiles == 1) hipLaunchKernelGGL((attention_shared_kernel<T, KC, 1, EXACT>), grid, threads, 0, stream, in);
+    else if (plan.apart && plan.tiles == 1) hipLaunchKernelGGL((attention_tiles_kernel<T, KC, 1, 4, EXACT>), grid, threads, 0, stream, in);
+    else if constexpr (KC <= 4) {
+        if (!plan.apart) hipLaunchKernelGGL((attention_shared_kernel<T, KC, 2, EXACT>), grid, threads, 0, stream, in);
+        else hipLaunchKernelGGL((attention_tiles_kernel<T, KC, 2, 8, EXACT>), grid, threads, 0, stream, in);
     }
-    else if (plan.tiles == 1) hipLaunchKernelGGL((attention_shared_kernel<T, KC, 1, EXACT>), grid, threads, 0, stream, in);
-    else if (plan.tiles == 2) hipLaunchKernelGGL((attention_shared_kernel<T, KC, 2, EXACT>), grid, threads, 0, stream, in);
-    else if constexpr (MOST == 4) hipLaunchKernelGGL((attention_shared_kernel<T, KC, 4, EXACT>), grid, threads, 0, stream, in);
     HIP_TRY(hipGetLastError());
     if (in.parts) {
         const long long all = in.n * in.at.m * in.heads * (in.at.d / 4);       // few, or the places would not be divided

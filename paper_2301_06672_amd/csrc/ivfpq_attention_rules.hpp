@@ -19,11 +19,14 @@ constexpr int kMostPartsEach = 64;    // of a sequence, on average: what is join
 
 inline AttentionPlan attention_plan(int64_t n, int m, int heads, int kv_heads, int d, int64_t max_places) {
     const int64_t columns = (int64_t)m * (heads / kv_heads);
-    const int most = d > 128 ? 2 : 4;                               // tiles whose sums fit a wave's registers
     AttentionPlan p{};
-    p.apart = columns > 16 * most;
-    p.tiles = p.apart ? 2 : columns <= 16 ? 1 : columns <= 32 ? 2 : most;
+    // Waves share up to 32 columns, 16 of long heads, whose sums leave room in the registers for keys and values on their way.  (12 rows of 8 sequences of
+    // up to 4,000 places, 32 heads over 8: 48 columns shared 63 us, apart 39; 24 rows of 128 components 62 with two tiles a wave and one block, 55 with one tile and
+    // two blocks; of 256 components, 64 rows 254 with two tiles a wave, 158 with one.  8 rows, 32 columns: shared 48 of those and 158 of 32 sequences of up
+    // to 8,000 places, apart 38 and 178.)
+    p.apart = columns > (d > 128 ? 16 : 32);
     p.waves = p.apart && columns > 128 && d <= 128 ? 8 : 4;
+    p.tiles = p.apart ? (p.waves == 8 ? 2 : 1) : columns <= 16 ? 1 : 2;
     p.blocks = (int)((columns + p.columns() - 1) / p.columns());
     // where sequences are too few to fill the GPU: parts for every CU twice over, of two tiles a wave at least.  They are equal whatever the lengths.
     // The kernel of eight waves leaves room for one workgroup on a CU: a part for each of one sequence, and of several, whose pieces differ, two rounds
