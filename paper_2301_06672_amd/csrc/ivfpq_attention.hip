@@ -5,8 +5,8 @@
 //
 // The rows of the heads that share keys are columns of two matrix products, S = K Q^T and O = V^T W^T, with 16 x 16 x 32 instructions: a tile is
 // 32 places and 16 columns.  Keys are dealt to the rows of the first product so that its results are, lane by lane, the operand of the
-// second (place 8 g + j of a tile is with lane group g in both), and the cache holds the values of 8 places side by side: nothing goes
-// through the LDS between the cache and the sums.
+// second (place 8 g + j of a tile is with lane group g in both), and the cache holds the values of 8 places side by side, so weights stay where they are
+// formed and every operand is read in 16-byte pieces.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -411,7 +411,8 @@ __device__ inline u32x4 held_fields(bool there, int first_place, long long place
 }
 
 // Few columns: the four waves share them, take every fourth tile, and add up at the end.  Keys and values come from the cache into registers, the next
-// tile's as soon as this one's are used.
+// tile's as soon as this one's are used: every byte of the cache is read once.  Bound by HBM: one row of 32 sequences of up to 16,384 places, 32 heads of 128 over
+// 8, 257 us (1.35 GB, 5.3 TB/s of the 5.6 that a plain read reaches).
 template <class T, int KC, int NQ, bool EXACT>
 __global__ __launch_bounds__(kAttentionThreads) void attention_shared_kernel(AttentionIn in) {
     constexpr int VT = KC * 2, STEP = 4;
@@ -517,10 +518,16 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_shared_kernel(Att
     if (wave == 0) cols.write(in, p.s, p.head, p.block, p.slot, p.block * NQ * 16, d, lane);
 }
 
-// Many columns: each wave has its own and goes over all tiles, which pass through the LDS, `AT_ONCE` at a time (what is done once for two is a third of
-// the instructions for one).  A tile is 4 KC operands of a wave, 1 KB each in the order of the lanes, so that they come and go in whole
-// lines: 2 KC of keys, then 2 KC of values.  A wave brings MINE of them: from the cache into registers three steps before they are used, into the LDS two steps
-// before; the next tile's keys are read from there while this one's scores become weights.
+// Many columns: each wave has its own and goes over all tiles, which pass through the LDS, AT_ONCE between two barriers.  A tile is 4 KC operands of a wave, 1 KB
+// each in the order of the lanes, so that they come and go in whole lines: 2 KC of keys, then 2 KC of values.  A wave brings MINE of them: from the
+// cache into registers three steps before they are used, into the LDS two steps before; the next tile's keys are read from there while this one's scores
+// become weights.
+//
+// 1,024 rows over 7,001 places, 32 heads of 128 over 8, 145 us: 875 TFLOP/s of the 1,430 of the library's product of 8,192^3.  With eight waves of 32 columns a tile
+// takes a CU 2,900 clocks, 1,024 of them matrix instructions (counters: the vector ALU is busy 1,450, and waves wait for barriers, the LDS and each other).  Four
+// waves of 64 columns (half the LDS reads) do not fit the registers: what is scaled now and then has to be where matrix instructions do not keep
+// it, and moves cost more.  Two phases a tile, half of the waves one behind: 175 us and no room for the masked tiles.  Left out in copies: exponentials -15 us, half of
+// the second product -30, the cache -16.
 template <class T, int KC, int NQ, int WAVES, bool EXACT>
 __global__ __launch_bounds__(64 * WAVES) void attention_tiles_kernel(AttentionIn in) {
     constexpr int VT = KC * 2, PARTS = 4 * KC, MINE = PARTS / WAVES, AT_ONCE = WAVES == 8 ? 2 : 1;
