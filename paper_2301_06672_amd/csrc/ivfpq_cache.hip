@@ -48,7 +48,7 @@ __device__ inline void load8(const T* p, bool pieces, float (&x)[8]) {
 constexpr int kAppendThreads = 256;
 
 // One workgroup for the rows whose places are one granule of 8: their values go to the cache as whole 16-byte pieces, and an angle is
-// formed once for all heads.  Bound by HBM with prompts (10,235 rows of 32 + 2 x 8 heads of 128, 161 MB in and out, 40 us; a copy of that takes 34), by latency with single
+// formed once for all heads.  Bound by HBM with prompts (6,552 rows of 32 + 2 x 8 heads of 128, 161 MB in and out, 40 us; a copy of that takes 34), by latency with single
 // tokens (64 of them 6 us).
 template <class T, class C>
 __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendIn in) {
