@@ -391,7 +391,8 @@ int ivfpq_distill_topk_step(const void* d_logits, int32_t dtype, int64_t n, int3
  *  - d_pages [n][max_pages] int32: place p of sequence s is place p % page of page d_pages[s][p / page].  d_lens [n] int32: places that
  *    the sequence has in the cache before the pass (negative values count as 0); row i is at place lens + i.  A place beyond max_pages pages, or in a
  *    page outside [0, n_pages), is not there: nothing is written to it and nothing read.  max_pages * page < 2^31 - 2^21.
- *  - The pages that hold a pass's rows belong to one sequence only. */
+ *  - The pages that hold a pass's rows belong to one sequence only, and stand once in its list.  Outputs overlap no inputs.
+ *  - Limits: n <= 2^20, n * m <= 2^24, kv_heads <= 4096, heads <= 65536. */
 enum {
     IVFPQ_MAX_DRAFT = 64,       /* rows of a tree */
     IVFPQ_MAX_DRAFT_DEPTH = 15, /* tokens of a continuation */
@@ -435,8 +436,9 @@ int ivfpq_cache_append(const void* d_q, int64_t q_stride, int32_t heads, const v
  *   d_q [n * m][heads][d] of the cache's type, 16-byte aligned, q_stride values from one row to the next, a multiple of 8; heads a multiple of kv_heads:
  *   head h reads the keys and values of h / (heads / kv_heads).  d_out [n * m][heads][d] likewise, out_stride, 8-byte aligned.  d_lse [n * m][heads]
  *   fp32, may be NULL.
- *   max_places: no sequence has more places with its rows (later ones are not looked at); it decides how the work is divided only.
+ *   max_places: no sequence has more places with its rows (pages behind them are not looked at); it decides how the work is divided only.
  *   Probabilities are fp32; they are rounded to the cache's type as factors of the values (the sum that divides them is of unrounded ones).
+ *   n * m * heads <= 2^26; the launch is limited to 2^23 workgroups.
  * d_workspace: >= ivfpq_draft_attention_workspace_bytes(...) (may be 0), 256-byte aligned. */
 size_t ivfpq_draft_attention_workspace_bytes(int64_t n, int32_t m, int32_t heads, int32_t kv_heads, int32_t d, int64_t max_places);
 int ivfpq_draft_attention(const void* d_q, int64_t q_stride, int32_t heads, int64_t n, int32_t m, const int32_t* d_parents,
@@ -460,6 +462,7 @@ int ivfpq_draft_attention(const void* d_q, int64_t q_stride, int32_t heads, int6
  *   d_path [n][m] int32: the kept rows, 0 first; then -1.  d_kept [n] int32: how many; 0 for a sequence without used rows.
  *   d_next [n] int32: the token behind the last kept row; -1 without used rows, and where that row has no distribution or NaN statistics
  *   d_logprobs [n][m] fp32: log p of the token behind each kept row (NaN in a row of NaN statistics); -inf in unused places.
+ * 1e-6 <= temperature <= 1e6; n * m <= 2^20, vocab <= 2^30, and n * m times the 2048s in vocab + 7 <= 2^24.
  * d_workspace: >= ivfpq_verify_drafts_workspace_bytes(...), 256-byte aligned; with_drafts: d_draft_logits is given. */
 size_t ivfpq_verify_drafts_workspace_bytes(int64_t n, int32_t m, int32_t vocab, int32_t with_drafts);
 int ivfpq_verify_drafts(const void* d_logits, int32_t dtype, int64_t n, int32_t m, int32_t vocab, int64_t row_stride,
@@ -470,7 +473,7 @@ int ivfpq_verify_drafts(const void* d_logits, int32_t dtype, int64_t n, int32_t 
 
 /* The kept rows move up behind each other: place lens + d_path[s][i] goes to lens + i, i < d_kept[s], in every layer.
  * d_path [n][m] int32, ascending, d_kept [n] int32 as ivfpq_verify_drafts gives them: entries outside [i, m) move nothing.
- * d_k_cache, d_v_cache: layers caches behind each other (all with the same pages).  The sequence's length is the caller's to raise by d_kept. */
+ * d_k_cache, d_v_cache: layers caches behind each other (all with the same pages); layers <= 4096, layers * kv_heads * d <= 2^31.  The sequence's length is the caller's to raise by d_kept. */
 int ivfpq_cache_keep(void* d_k_cache, void* d_v_cache, int32_t cache_dtype, int32_t layers, int64_t n_pages, int32_t kv_heads, int32_t page,
                      int32_t d, const int32_t* d_pages, int32_t max_pages, const int32_t* d_lens, int64_t n, int32_t m,
                      const int32_t* d_path, const int32_t* d_kept, void* hip_stream);

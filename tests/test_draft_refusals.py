@@ -68,7 +68,7 @@ CASES = (
         [({name: 0}, "EINVAL", "null") for name in ("logits", "tokens", "path", "kept", "following", "logprobs")]]
     + [("ivfpq_cache_keep", KEEP, *c) for c in CACHES + [
         (dict(layers=0), "EINVAL", "layers"), (dict(layers=4097), "EINVAL", "layers"), (dict(path=0), "EINVAL", "null"), (dict(kept=0), "EINVAL", "null"),
-        (dict(n=1, m=(1 << 20) + 1), "EUNSUPPORTED", "m=")]]
+        (dict(layers=4096, kv_heads=4096, d=256), "EUNSUPPORTED", "components"), (dict(n=1, m=(1 << 20) + 1), "EUNSUPPORTED", "m=")]]
 )
 
 
