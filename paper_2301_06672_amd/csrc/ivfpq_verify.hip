@@ -61,7 +61,7 @@ __device__ inline float maximum3(float a, float b, float c) {       // NaN if on
     return d;
 }
 
-// 2^y for y <= 0, right to 1.1 10^-12; what is under 2^-1000 may be anything down to 0
+// 2^y for y <= 1/2, right to 1.1 10^-12; what is under 2^-1000 may be anything down to 0
 __device__ inline double exp2_exact(double y) {
     y = fmax(y, -1100.0);
     const double n = rint(y), f = y - n;
@@ -76,22 +76,36 @@ __device__ inline double exp2_exact(double y) {
     p = fma(p, f, 1.0);
     return __builtin_amdgcn_ldexp(p, (int)n);
 }
-// The same for -1023 < y <= 0.  The nearest whole number comes from an addition that leaves it in the low bits.
-// The coefficients stay in vector registers: an operation takes one from a scalar register at most, and a copy of it costs as much as half of one.
+// 2^(i / 32)
+__device__ const double kExp2Table[32] = {
+    0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0, 0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0,
+    0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0, 0x1.306fe0a31b715p+0, 0x1.371a7373aa9cbp+0, 0x1.3dea64c123422p+0, 0x1.44e086061892dp+0,
+    0x1.4bfdad5362a27p+0, 0x1.5342b569d4f82p+0, 0x1.5ab07dd485429p+0, 0x1.6247eb03a5585p+0, 0x1.6a09e667f3bcdp+0, 0x1.71f75e8ec5f74p+0,
+    0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0, 0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0, 0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0,
+    0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0};
+// 2^(y / 32) in fewer instructions, right to 10^-13, from the nearest whole number of y and the rest: 2^(n + i / 32 + f / 32) with 2^(i / 32) from a table in
+// the LDS, n added to its exponent, and a polynomial of degree 4 for the rest, |f| <= 1/2.  An addition leaves the nearest whole number in the low bits.
+// The coefficients stay in vector registers: an operation takes one from a scalar register at most, and a copy of it costs as much as the operation.
+constexpr int kExp2Steps = 32;
+constexpr double kWhole = 0x1.8p52;
+__device__ inline int low_word(double x) { return __builtin_bit_cast(int2, x).x; }
 struct Exp2Terms {
-    double c[9] = {1.0, 0x1.62e42fef84cf0p-1, 0x1.ebfbdff823cedp-3, 0x1.c6b08dd6fd236p-5, 0x1.3b2ab7181b778p-7, 0x1.5d8745a72827ap-10, 0x1.4308ac85a6c21p-13,
-                   0x1.00dc4a534054dp-16, 0x1.63d1363a7ecb6p-20};
-    __device__ inline Exp2Terms() {
+    const double* steps;                              // 2^(i / 32) less i 2^15 in the high word, which n 2^20 + i 2^15 is added to
+    double c[5] = {1.0, 0x1.62e42fef6d01ap-6, 0x1.ebfbdff8131c3p-13, 0x1.c6b167e571135p-20, 0x1.3b2b1bee88b09p-27};
+    __device__ inline Exp2Terms(const double* steps) : steps(steps) {
 #pragma unroll
-        for (int i = 0; i < 9; ++i) asm("" : "+v"(c[i]));
+        for (int i = 0; i < 5; ++i) asm("" : "+v"(c[i]));
     }
-    __device__ inline double operator()(double y) const {
-        constexpr double kWhole = 0x1.8p52;
-        const double shifted = y + kWhole, f = y - (shifted - kWhole);
-        double p = c[8];
+    // sum + 2^((whole + f) / 32), -32700 < whole < 32700
+    __device__ inline double add(int whole, double f, double sum) const {
+        int2 step = __builtin_bit_cast(int2, steps[whole & (kExp2Steps - 1)]);
+        asm("" : "+v"(step.y));                       // or else the sum is made of 64 bits, in five instructions
+        step.y = (int)(((unsigned)whole << 15) + (unsigned)step.y);
+        double p = c[4];
 #pragma unroll
-        for (int i = 7; i >= 0; --i) p = fma(p, f, c[i]);
-        return __builtin_amdgcn_ldexp(p, __builtin_bit_cast(int2, shifted).x);
+        for (int i = 3; i >= 0; --i) p = fma(p, f, c[i]);
+        return fma(p, __builtin_bit_cast(double, step), sum);
     }
 };
 // exp((x - most) / T); `most` is finite
@@ -162,14 +176,63 @@ struct BlockChunks {
     }
 };
 
+// The largest and the smallest of a lane's values.  (Where the smallest is not too far down, no term of the sum has to be looked at for that.)  16-bit ones are compared two at a time as whole numbers: as signed ones the largest is right if it is not
+// negative, as unsigned ones the smallest is the largest if all have a sign, and the largest the smallest if one has.
+template <class T>
+struct Extent {
+    float most, least;                                // most: NaN if a value is
+    __device__ inline Extent(const BlockChunks<T>& held) {
+        if constexpr (sizeof(T) == 2) {
+            typedef int16_t s2 __attribute__((ext_vector_type(2)));
+            typedef uint16_t u2 __attribute__((ext_vector_type(2)));
+            constexpr unsigned kInf = std::is_same<T, half_t>::value ? 0x7C00 : 0x7F80;
+            s2 top = __builtin_bit_cast(s2, held.chunk[0].bits.x);
+            u2 high = __builtin_bit_cast(u2, top), low = high;
+#pragma unroll
+            for (int i = 0; i < held.N; ++i) {
+                const uint4 bits = held.chunk[i].bits;
+                const uint32_t words[4] = {bits.x, bits.y, bits.z, bits.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    top = __builtin_elementwise_max(top, __builtin_bit_cast(s2, words[j]));
+                    high = __builtin_elementwise_max(high, __builtin_bit_cast(u2, words[j]));
+                    low = __builtin_elementwise_min(low, __builtin_bit_cast(u2, words[j]));
+                }
+            }
+            const int largest = max(top.x, top.y);
+            const unsigned highest = max(high.x, high.y), lowest = min(low.x, low.y);
+            const auto value = [](unsigned bits) { return (float)__builtin_bit_cast(T, (uint16_t)bits); };
+            most = highest > (0x8000 | kInf) ? NAN : value(largest >= 0 ? (unsigned)largest : lowest);
+            least = value(highest >= 0x8000 ? highest : lowest);
+        } else {
+            most = -INFINITY, least = INFINITY;
+#pragma unroll
+            for (int i = 0; i < held.N; ++i) {
+                float x[4];
+                held.chunk[i].widen(x);
+                most = maximum3(maximum3(most, x[0], x[1]), x[2], x[3]);
+                least = fminf(fminf(least, fminf(x[0], x[1])), fminf(x[2], x[3]));
+            }
+        }
+    }
+};
+
 constexpr int kSumThreads = 256;
 
-// The blocks' sums of all used rows, a wave a block.  Bound by 64-bit arithmetic: some 18 operations a value, 5 clocks of a SIMD each (1,024 rows of 65,536 bf16
-// logits, 134 MB, in 52 us, of which those operations are 36 at least; four blocks a wave, the next one's logits on their way: 54).
+// The blocks' sums of all used rows, a wave a block.  Bound by vector instructions, 4 clocks of a SIMD each whether of 32 bits or of 64 (counters: busy all the time with
+// 730 a wave): 1.5 a value to the extremes, 14 to the sum.  1,024 rows of 65,536 bf16 logits, 134 MB, take 42 us, 24 to read; with a polynomial of degree 8
+// in place of the table and every value held above a bound 51.  A table for each wave, filled while the logits are on their way: 45.
 template <class T>
-__global__ __launch_bounds__(kSumThreads) void block_sums_kernel(VerifyIn in) {
+__global__ __launch_bounds__(kSumThreads, sizeof(T) == 2 ? 8 : 5) void block_sums_kernel(VerifyIn in) {
     constexpr int VEC = Chunk<T>::VEC;
+    __shared__ double steps[kExp2Steps];
     const int lane = threadIdx.x & 63;
+    if (threadIdx.x < kExp2Steps) {
+        int2 step = __builtin_bit_cast(int2, kExp2Table[threadIdx.x]);
+        step.y -= (int)threadIdx.x << 15;
+        steps[threadIdx.x] = __builtin_bit_cast(double, step);
+    }
+    __syncthreads();
     // 2^25 blocks of 2^21 rows at most; divisions of 64 bits would take as long as a third of the sums
     const unsigned item = __builtin_amdgcn_readfirstlane(blockIdx.x * (kSumThreads / 64) + (threadIdx.x >> 6));
     const unsigned row = item / (unsigned)in.row_blocks, targets = (unsigned)(in.n * in.m);
@@ -183,38 +246,41 @@ __global__ __launch_bounds__(kSumThreads) void block_sums_kernel(VerifyIn in) {
     const RowChunks<T> values(draft ? in.drafts : in.logits, r, draft ? in.draft_stride : in.stride, in.vocab);
     if (block * kBlock >= values.end) return;
     BlockChunks<T> held(values, block, lane);
-    float most = -INFINITY;
+    const Extent<T> extent(held);
 #pragma unroll
-    for (int i = 0; i < held.N; ++i) {
-        float x[VEC];
-        held.chunk[i].widen(x);
-#pragma unroll
-        for (int e = 0; e < VEC; e += 2) most = maximum3(most, x[e], x[e + 1]);
-        held.chunk[i].forget_widened();
-    }
-    most = wave_maximum(most);
+    for (int i = 0; i < held.N; ++i) held.chunk[i].forget_widened();
+    const float most = wave_maximum(extent.most);
     double sum = 0.0;
     if (most > -INFINITY && most < INFINITY) {
-        const Exp2Terms power;
-        const auto add_up = [&](auto&& exponent) {
+        const Exp2Terms power(steps);
+        const double scale = in.scale * kExp2Steps;
+        const auto add_up = [&](auto&& add) {
             double sums[2] = {0.0, 0.0};
 #pragma unroll
             for (int i = 0; i < held.N; ++i) {
                 float x[VEC];
                 held.chunk[i].widen(x);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) sums[e & 1] += power(exponent(x[e]));
+                for (int e = 0; e < VEC; ++e) sums[e & 1] = add((double)x[e], sums[e & 1]);
             }
             return wave_sum(sums[0] + sums[1]);
         };
-        const double less = (double)most * in.scale;
-        if (fabs(less) < 0x1p30) {
-            // x scale - most scale in one operation; what the second product loses, under 2^-23, is a factor of the whole block.  What is under 2^-1000,
-            // of a logit of -inf too, is taken for that: lost in a sum that holds a 1
-            const float least = (float)((double)most - 1000.0 / in.scale);
-            const double lost = fma((double)most, in.scale, -less) * 0.6931471805599453;
-            sum = add_up([&](float x) { return fma((double)fmaxf(x, least), in.scale, -less); }) * (1.0 - lost + 0.5 * lost * lost);
-        } else sum = add_up([&](float x) { return fmax(((double)x - (double)most) * in.scale, -1000.0); });
+        const double whole_most = rint((double)most * scale);
+        if (fabs(whole_most) < 0x1p30 && __all(((double)extent.least - (double)most) * scale > -32000.0)) {
+            // x scale = r + f; r less that of the largest is in the low bits, and what the largest had of f is a factor of the whole block
+            const double magic = kWhole - whole_most;
+            sum = add_up([&](double x, double sum) {
+                const double shifted = fma(x, scale, magic);
+                return power.add(low_word(shifted), fma(x, scale, magic - shifted), sum);
+            });
+            sum *= exp2_exact(fma((double)most, scale, -whole_most) * (-1.0 / kExp2Steps));
+        } else {
+            // what is under 2^-1000, of a logit of -inf too, is taken for that: lost in a sum that holds a 1
+            sum = add_up([&](double x, double sum) {
+                const double y = fmax((x - (double)most) * scale, -32000.0), shifted = y + kWhole;
+                return power.add(low_word(shifted), y - (shifted - kWhole), sum);
+            });
+        }
     }
     if (lane == 0) in.blocks[item] = BlockSum{sum, most, 0};
 }

@@ -209,6 +209,40 @@ def test_masks_and_lowest_values(P):
         assert got.next_tokens.tolist()[0] == 6_199 and got.next_tokens.tolist()[3] == vocab - 1
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("middle,size,temperature", [(0.0, 3.0, 1.0), (-100.0, 1.0, 1.0), (100.0, 1.0, 1.0), (-100.0, 1.0, 0.01), (100.0, 1.0, 0.01), (0.0, 3.0, 1e6),
+                                                     (1e4, 1.0, 1e-6), (-1e4, 1.0, 1e-6)])
+def test_signs_and_spreads(P, dtype, middle, size, temperature):
+    """All values of one sign, of both; some far under the largest, so that their weights are cut off, in some blocks of a row only; sums about numbers that no
+    longer fit 2^30 steps of 1/32.  (Shares of 64 bits are right to 10^-11 in the plain form up to 10^4 temperatures; beyond, logits here are equal or far apart.)"""
+    n, m, vocab = 2, 4, 9_001
+    logits, gen = rows(n, m, vocab, torch.float32, 31, size)
+    logits += middle
+    logits[0, 2_500:2_510] = middle - 2_000.0
+    logits[1, ::2] = middle - 900.0
+    logits[2, 4_100:] = -math.inf
+    logits = logits.to(dtype)
+    parents, tokens = likely_tree(logits, n, m, gen)
+    for uniforms in (torch.rand(n, m, generator=gen), None):
+        check(P, logits, tokens, parents, uniforms=uniforms, temperature=temperature)
+
+
+@pytest.mark.parametrize("dtype,bits", [(torch.float32, 0xFFC00000 - (1 << 32)), (torch.float16, 0xFE00 - (1 << 16)), (torch.bfloat16, 0xFFC0 - (1 << 16))])
+def test_nan_of_either_sign(P, dtype, bits):
+    n, m, vocab = 3, 1, 5_000
+    logits, gen = rows(n, m, vocab, dtype, 32)
+    as_whole = torch.int32 if dtype == torch.float32 else torch.int16
+    logits.view(as_whole)[0, 4_999] = bits                               # the sign set
+    logits[1, 2_047] = math.nan
+    logits[0, 0] = -1.0
+    assert math.isnan(float(logits[0, 4_999]))
+    tokens = torch.zeros(n, m, dtype=torch.int32)
+    for uniforms in (torch.rand(n, m, generator=gen), None):
+        assert check(P, logits, tokens, uniforms=uniforms).next_tokens.tolist()[:2] == [-1, -1]
+    logits = -logits.abs()                                               # and with nothing but signs set
+    check(P, logits, tokens, uniforms=torch.rand(n, m, generator=gen))
+
+
 def test_bad_parents_and_tokens(P):
     """Parents out of range follow the cache and are never reached from a row; tokens out of range are never said."""
     n, m, vocab = 2, 6, 50
