@@ -17,6 +17,8 @@ namespace {
 constexpr int kMostDraft = IVFPQ_MAX_DRAFT;
 constexpr int kBlock = 2048;                          // values of a block, one wave's work: 32 a lane
 constexpr int kLaneValues = kBlock / 64;
+constexpr int kLeftBlock = 512;                       // of what a draft leaves of a distribution: few rows, so more waves for each
+constexpr int kLeftValues = kLeftBlock / 64;
 
 // What is kept of a block: the sum of exp((x - most) / T).  NaN and +inf stay in `most`.
 struct BlockSum {
@@ -51,7 +53,8 @@ struct VerifyIn {
 // Where a sequence's chain ends: the row whose distribution the next token comes from, and what normalises it and its draft's.
 struct Stop {
     float most, draft_most;
-    double total, draft_total;                        // 0: no distribution
+    double total;                                     // 0: no distribution
+    double of_total, of_draft;                        // 1 by it and by the draft's
     int row, drafted;                                 // row -1: no used rows; drafted: less the draft's probabilities
 };
 
@@ -350,11 +353,12 @@ __device__ inline Picked pick_block(int count, double share, int lane, Of&& of) 
 }
 
 // The lowest of a block's tokens whose running sum, with what is before the block, is over the target; -1 if all weigh nothing.  A lane has
-// kLaneValues tokens in a row: their weights w, that lie from token `first` of the row on.
-__device__ inline int pick_token(const double (&w)[kLaneValues], int first, const Picked& picked) {
+// N tokens in a row: their weights w, that lie from token `first` of the row on.
+template <int N>
+__device__ inline int pick_token(const double (&w)[N], int first, const Picked& picked) {
     double mine = 0.0;
 #pragma unroll
-    for (int i = 0; i < kLaneValues; ++i) mine += w[i];
+    for (int i = 0; i < N; ++i) mine += w[i];
     double base = picked.before;
     const Crossing c = cross(mine, picked.target, base);
     if (c.lane < 0) return -1;
@@ -362,7 +366,7 @@ __device__ inline int pick_token(const double (&w)[kLaneValues], int first, cons
     int token = -1;
     bool over = false;
 #pragma unroll
-    for (int i = 0; i < kLaneValues; ++i) {
+    for (int i = 0; i < N; ++i) {
         at += w[i];
         if (w[i] > 0.0 && !over) {
             token = first + i;                        // the last one, where rounding leaves all under the target
@@ -532,26 +536,26 @@ __global__ __launch_bounds__(kWalkThreads) void verify_chain_kernel(VerifyIn in)
             to.total = norms[stop].total;
             to.drafted = stop + 1 < count && draft_norms[stop].total > 0.0;
             to.draft_most = draft_norms[stop].most;
-            to.draft_total = draft_norms[stop].total;
+            to.of_total = 1.0 / norms[stop].total;
+            to.of_draft = 1.0 / draft_norms[stop].total;
         }
         in.stops[s] = to;
     }
 }
 
-// max(p - q, 0) of kLaneValues tokens, STEP apart, of the row where a chain ends; 0 behind the vocabulary
+// max(p - q, 0) of kLeftValues tokens, STEP apart, of the row where a chain ends; 0 behind the vocabulary
 template <int STEP, class T>
-__device__ inline void left_weights(const Stop& stop, const T* logits, const T* drafts, int first, const VerifyIn& in, double (&w)[kLaneValues]) {
-    const double of_p = 1.0 / stop.total, of_q = 1.0 / stop.draft_total;
-    T x[kLaneValues], y[kLaneValues];
+__device__ inline void left_weights(const Stop& stop, const T* logits, const T* drafts, int first, const VerifyIn& in, double (&w)[kLeftValues]) {
+    T x[kLeftValues], y[kLeftValues];
 #pragma unroll
-    for (int i = 0; i < kLaneValues; ++i) {
+    for (int i = 0; i < kLeftValues; ++i) {
         const int token = min(first + i * STEP, in.vocab - 1);
         x[i] = logits[token];
         y[i] = drafts[token];
     }
 #pragma unroll
-    for (int i = 0; i < kLaneValues; ++i) {
-        const double p = weight((float)x[i], stop.most, in.scale) * of_p, q = weight((float)y[i], stop.draft_most, in.scale) * of_q;
+    for (int i = 0; i < kLeftValues; ++i) {
+        const double p = weight((float)x[i], stop.most, in.scale) * stop.of_total, q = weight((float)y[i], stop.draft_most, in.scale) * stop.of_draft;
         w[i] = first + i * STEP < in.vocab ? fmax(p - q, 0.0) : 0.0;
     }
 }
@@ -560,22 +564,24 @@ __device__ inline const T* draft_row(const VerifyIn& in, long long s, int i) {
     return (const T*)in.drafts + (s * (in.m - 1) + i) * in.draft_stride;
 }
 
-// The sums of max(p - q, 0) over blocks of the rows where chains end, a wave a block: 33 rows of 131,071 in 10 us, 19 with a lane's tokens in a row.
+// The sums of max(p - q, 0) over blocks of the rows where chains end, a wave a block: 33 rows of 131,071 in 9.6 us (10 with blocks of 2048, whose 32 tokens a lane then
+// take the draw 6.7 us in place of 5.6; 19 with a lane's tokens in a row).  Half of that are its vector instructions, 36 a token.
 template <class T>
 __global__ __launch_bounds__(kSumThreads) void left_sums_kernel(VerifyIn in) {
     const int lane = threadIdx.x & 63;
-    const long long item = (long long)blockIdx.x * (kSumThreads / 64) + (threadIdx.x >> 6);
-    const long long s = item / in.left_blocks;
-    const int block = (int)(item % in.left_blocks);
+    // fewer than 2^26; a division of 64 bits and those of the totals would take longer than the block
+    const unsigned item = __builtin_amdgcn_readfirstlane(blockIdx.x * (kSumThreads / 64) + (threadIdx.x >> 6));
+    const long long s = item / (unsigned)in.left_blocks;
+    const int block = (int)(item - (unsigned)s * in.left_blocks);
     if (s >= in.n) return;
     const Stop stop = in.stops[s];
     if (stop.row < 0 || !stop.drafted || !(stop.total > 0.0)) return;
     const T* x = (const T*)in.logits + (s * in.m + stop.row) * in.stride;
     const T* y = draft_row<T>(in, s, stop.row);
-    double w[kLaneValues], sum = 0.0;
-    left_weights<64>(stop, x, y, block * kBlock + lane, in, w);
+    double w[kLeftValues], sum = 0.0;
+    left_weights<64>(stop, x, y, block * kLeftBlock + lane, in, w);
 #pragma unroll
-    for (int i = 0; i < kLaneValues; ++i) sum += w[i];
+    for (int i = 0; i < kLeftValues; ++i) sum += w[i];
     sum = wave_sum(sum);
     if (lane == 0) in.left[s * in.left_blocks + block] = sum;
 }
@@ -600,9 +606,9 @@ __global__ __launch_bounds__(64) void draw_left_kernel(VerifyIn in) {
         const Picked picked = pick_block(in.left_blocks, u, lane, [&](int b) { return left[b]; });
         if (picked.block >= 0) {
             const T* x = (const T*)in.logits + flat * in.stride;
-            double w[kLaneValues];
-            left_weights<1>(stop, x, draft_row<T>(in, s, stop.row), picked.block * kBlock + lane * kLaneValues, in, w);
-            token = pick_token(w, picked.block * kBlock + lane * kLaneValues, picked);
+            double w[kLeftValues];
+            left_weights<1>(stop, x, draft_row<T>(in, s, stop.row), picked.block * kLeftBlock + lane * kLeftValues, in, w);
+            token = pick_token(w, picked.block * kLeftBlock + lane * kLeftValues, picked);
             if (token >= 0) logit = (float)x[token];
         }
     }
@@ -616,7 +622,7 @@ __global__ __launch_bounds__(64) void draw_left_kernel(VerifyIn in) {
 // ---- launches
 
 int row_blocks(int32_t vocab) { return (int)(((int64_t)vocab + 7 + kBlock - 1) / kBlock); }      // at the worst alignment
-int left_blocks(int32_t vocab) { return (int)(((int64_t)vocab + kBlock - 1) / kBlock); }
+int left_blocks(int32_t vocab) { return (int)(((int64_t)vocab + kLeftBlock - 1) / kLeftBlock); }
 
 struct VerifySpace {
     size_t blocks, left, stops, said;
@@ -656,8 +662,10 @@ int launch_verify(const VerifyIn& in, hipStream_t stream) {
     }
     hipLaunchKernelGGL((verify_chain_kernel<T>), dim3((unsigned)in.n), dim3(kWalkThreads), 0, stream, in);
     HIP_TRY(hipGetLastError());
-    hipLaunchKernelGGL((left_sums_kernel<T>), dim3((unsigned)((in.n * in.left_blocks + kWaves - 1) / kWaves)), dim3(kSumThreads), 0, stream, in);
-    HIP_TRY(hipGetLastError());
+    if (in.m > 1) {                                    // else nothing was drafted.  A row of two at least: fewer than 2^26 waves
+        hipLaunchKernelGGL((left_sums_kernel<T>), dim3((unsigned)((in.n * in.left_blocks + kWaves - 1) / kWaves)), dim3(kSumThreads), 0, stream, in);
+        HIP_TRY(hipGetLastError());
+    }
     hipLaunchKernelGGL((draw_left_kernel<T>), dim3((unsigned)in.n), dim3(64), 0, stream, in);
     HIP_TRY(hipGetLastError());
     return IVFPQ_OK;
