@@ -523,7 +523,7 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_shared_kernel(Att
 // cache into registers three steps before they are used, into the LDS two steps before; the next tile's keys are read from there while this one's scores
 // become weights.
 //
-// 1,024 rows over 7,001 places, 32 heads of 128 over 8, 136 us (145 after a pause): 930 TFLOP/s of the 1,430 of the library's product of 8,192^3.  With eight waves of 32 columns a tile
+// 1,024 rows over 7,001 places, 32 heads of 128 over 8, 137 us (160 after a pause): 920 TFLOP/s of the 1,430 of the library's product of 8,192^3.  With eight waves of 32 columns a tile
 // takes a CU 2,900 clocks, 1,024 of them matrix instructions (counters: the vector ALU is busy 1,450, and waves wait for barriers, the LDS and each other).  Four
 // waves of 64 columns (half the LDS reads) do not fit the registers: what is scaled now and then has to be where matrix instructions do not keep
 // it, and moves cost more.  Two phases a tile, half of the waves one behind: 175 us and no room for the masked tiles.  Left out in copies: exponentials -15 us, half of

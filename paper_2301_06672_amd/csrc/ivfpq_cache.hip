@@ -45,11 +45,12 @@ __device__ inline void load8(const T* p, bool pieces, float (&x)[8]) {
     }
 }
 
-constexpr int kAppendThreads = 256;
+constexpr int kAppendThreads = 256, kAppendAtOnce = 2;
 
 // One workgroup for the rows whose places are one granule of 8: their values go to the cache as whole 16-byte pieces, and an angle is
-// formed once for all heads.  Bound by HBM with prompts (6,552 rows of 32 + 2 x 8 heads of 128, 161 MB in and out, 40 us; a copy of that takes 34), by latency with single
-// tokens (64 of them 6 us).
+// formed once for all heads.  Bound by HBM with prompts (6,552 rows of 32 + 2 x 8 heads of 128, 161 MB in and out: 47 us, and 35 where the last-level cache holds
+// them; a copy of that takes 34.  One piece at once 50 and 38, four 68 and 48; divisions of indexes in the loop 56 and 45), by latency with single tokens (64 of
+// them 6 us).
 template <class T, class C>
 __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendIn in) {
     __shared__ float turns[8][kMostHead];           // cos, then sin, of each pair
@@ -61,82 +62,14 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendIn i
     const long long base = granule * 8 - len;
     const int first = (int)max(base, 0ll), used = (int)min(base + 8, (long long)count), all = (int)min(base + 8, (long long)m);
     if (first >= all) return;
-    const int half = in.rotated / 2;
-    for (int i = tid; i < (used - first) * half; i += kAppendThreads) {
-        const int row = first + i / half, pair = i % half;
-        const double position = (double)len + (double)(in.depths ? in.depths[s * m + row] : row);
-        double turn = position * (double)in.inv_freq[pair] * 0.15915494309189535;           // of 2 pi
-        turn -= rint(turn);
-        float sine, cosine;
-        sincosf((float)(turn * 6.283185307179586), &sine, &cosine);
-        turns[row - base][pair] = cosine * in.amplitude;
-        turns[row - base][half + pair] = sine * in.amplitude;
-    }
-    __syncthreads();
-
     const int pieces = d / 8;                       // of a head
     const int page = used > first ? in.at.page_of(s, granule * 8) : -1;
     const int off = (int)(granule * 8) & (in.at.page() - 1);
     C* k_page = (C*)in.k_cache + (page < 0 ? 0 : page) * in.at.page_values();
     C* v_page = (C*)in.v_cache + (page < 0 ? 0 : page) * in.at.page_values();
 
-    // queries, then keys: a piece of 8 components a thread
-    const int per_row = (in.heads + kv_heads) * pieces;
-    for (int i = tid; i < (all - first) * per_row; i += kAppendThreads) {
-        const int row = first + i / per_row, piece = i % per_row;
-        const int head = piece / pieces, c = piece % pieces * 8;
-        const bool query = head < in.heads;
-        const long long flat = s * m + row;
-        typedef C out_t __attribute__((ext_vector_type(8)));
-        out_t y;
-        if (row >= used) {
-            if (!query) continue;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = (C)0.f;
-        } else {
-            if (!query && page < 0) continue;
-            const bool whole = query ? in.q_pieces : in.k_pieces;
-            const T* x = query ? (const T*)in.q + flat * in.q_stride + (long long)head * d : (const T*)in.k + flat * in.k_stride + (long long)(head - in.heads) * d;
-            const float* turn = turns[row - base];
-            float a[8], b[8];
-            load8(x + c, whole, a);
-            if (c >= in.rotated) {
-            } else if (in.interleaved) {
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    const int pair = (c + j) / 2;
-                    if (c + j < in.rotated) {
-                        const float cosine = turn[pair], sine = turn[half + pair], p = a[j], r = a[j + 1];
-                        a[j] = p * cosine - r * sine;
-                        a[j + 1] = r * cosine + p * sine;
-                    }
-                }
-            } else if (half % 8 == 0) {
-                const bool low = c < half;
-                load8(x + (low ? c + half : c - half), whole, b);
-                const float* cosine = turn + (low ? c : c - half);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) a[j] = low ? a[j] * cosine[j] - b[j] * cosine[half + j] : a[j] * cosine[j] + b[j] * cosine[half + j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int e = c + j;
-                    if (e >= in.rotated) continue;
-                    const int pair = e < half ? e : e - half;
-                    const float other = (float)x[e < half ? e + half : e - half], cosine = turn[pair], sine = turn[half + pair];
-                    a[j] = e < half ? a[j] * cosine - other * sine : a[j] * cosine + other * sine;
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = (C)a[j];
-        }
-        C* to = query ? (C*)in.q_out + (flat * in.heads + head) * d + c : k_page + (((long long)(head - in.heads) << in.at.shift) + off + (row - base)) * d + c;
-        *reinterpret_cast<out_t*>(to) = y;
-    }
-
     // values: 8 components of the granule's rows a thread, turned over in registers
-    if (page < 0) return;
-    for (int i = tid; i < kv_heads * pieces; i += kAppendThreads) {
+    for (int i = tid; i < kv_heads * pieces && page >= 0; i += kAppendThreads) {
         const int head = i / pieces, c = i % pieces * 8;
         C* to = v_page + (((long long)head << in.at.shift) + off) * d + c * 8;
         const T* x = (const T*)in.v + (s * m + base) * in.v_stride + (long long)head * d + c;
@@ -164,6 +97,104 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendIn i
 #pragma unroll
                 for (int j = 0; j < 8; ++j) to[j * 8 + (row - base)] = (C)a[j];
             }
+        }
+    }
+
+    // angles
+    const int half = in.rotated / 2;
+    for (int i = tid; i < (used - first) * half; i += kAppendThreads) {
+        const int row = first + i / half, pair = i % half;
+        const double position = (double)len + (double)(in.depths ? in.depths[s * m + row] : row);
+        double turn = position * (double)in.inv_freq[pair] * 0.15915494309189535;           // of 2 pi
+        turn -= rint(turn);
+        float sine, cosine;
+        sincosf((float)(turn * 6.283185307179586), &sine, &cosine);
+        turns[row - base][pair] = cosine * in.amplitude;
+        turns[row - base][half + pair] = sine * in.amplitude;
+    }
+    __syncthreads();
+
+    // queries, then keys: a piece of 8 components a thread, with the one that it turns with where they lie apart, and kAppendAtOnce of those loaded at once.  A
+    // thread has the same components of other heads each time: divisions of every index would take as long as the memory.
+    typedef C out_t __attribute__((ext_vector_type(8)));
+    const bool apart = !in.interleaved && half > 0 && half % 8 == 0;
+    const int units = pieces - (apart ? half / 8 : 0), all_heads = in.heads + kv_heads, at_once = kAppendThreads / units;
+    int c = tid % units * 8, next_row = first, next_head = tid / units;
+    const bool two = apart && c < half;
+    if (apart && !two) c += half;
+    if (next_head >= at_once) return;
+    while (next_row < all) {
+        int rows[kAppendAtOnce], heads[kAppendAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAppendAtOnce; ++u) {
+            while (next_head >= all_heads && next_row < all) {
+                next_head -= all_heads;
+                ++next_row;
+            }
+            rows[u] = next_row;
+            heads[u] = next_head;
+            next_head += at_once;
+        }
+        float a[kAppendAtOnce][8], b[kAppendAtOnce][8];
+        const auto source = [&](int row, int head) {
+            const long long flat = s * m + row;
+            return head < in.heads ? (const T*)in.q + flat * in.q_stride + (long long)head * d : (const T*)in.k + flat * in.k_stride + (long long)(head - in.heads) * d;
+        };
+#pragma unroll
+        for (int u = 0; u < kAppendAtOnce; ++u) {
+            const int row = rows[u], head = heads[u];
+            if (row >= used || (head >= in.heads && page < 0)) continue;
+            const bool whole = head < in.heads ? in.q_pieces : in.k_pieces;
+            const T* x = source(row, head) + c;
+            load8(x, whole, a[u]);
+            if (two) load8(x + half, whole, b[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAppendAtOnce; ++u) {
+            const int row = rows[u], head = heads[u];
+            const bool query = head < in.heads, used_row = row < used;
+            if (row >= all || (!query && (!used_row || page < 0))) continue;
+            C* to = query ? (C*)in.q_out + ((s * m + row) * in.heads + head) * d + c : k_page + (((long long)(head - in.heads) << in.at.shift) + off + (row - base)) * d + c;
+            out_t y, z;
+            if (!used_row) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = z[j] = (C)0.f;
+            } else {
+                const float* turn = turns[row - base];
+                if (two) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float cosine = turn[c + j], sine = turn[half + c + j], p = a[u][j], r = b[u][j];
+                        a[u][j] = p * cosine - r * sine;
+                        z[j] = (C)(r * cosine + p * sine);
+                    }
+                } else if (apart || c >= in.rotated) {
+                } else if (in.interleaved) {
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) {
+                        const int pair = (c + j) / 2;
+                        if (c + j < in.rotated) {
+                            const float cosine = turn[pair], sine = turn[half + pair], p = a[u][j], r = a[u][j + 1];
+                            a[u][j] = p * cosine - r * sine;
+                            a[u][j + 1] = r * cosine + p * sine;
+                        }
+                    }
+                } else {
+                    const T* x = source(row, head);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int e = c + j;
+                        if (e >= in.rotated) continue;
+                        const int pair = e < half ? e : e - half;
+                        const float other = (float)x[e < half ? e + half : e - half], cosine = turn[pair], sine = turn[half + pair];
+                        a[u][j] = e < half ? a[u][j] * cosine - other * sine : a[u][j] * cosine + other * sine;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = (C)a[u][j];
+            }
+            *reinterpret_cast<out_t*>(to) = y;
+            if (two) *reinterpret_cast<out_t*>(to + half) = z;
         }
     }
 }
