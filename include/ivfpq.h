@@ -436,7 +436,8 @@ int ivfpq_cache_append(const void* d_q, int64_t q_stride, int32_t heads, const v
  *   d_q [n * m][heads][d] of the cache's type, 16-byte aligned, q_stride values from one row to the next, a multiple of 8; heads a multiple of kv_heads:
  *   head h reads the keys and values of h / (heads / kv_heads).  d_out [n * m][heads][d] likewise, out_stride, 8-byte aligned.  d_lse [n * m][heads]
  *   fp32, may be NULL.
- *   max_places: no sequence has more places with its rows (pages behind them are not looked at); it decides how the work is divided only.
+ *   max_places: about how many places the longest sequence has with its rows.  It decides how the work is divided and what workspace that needs, and nothing
+ *   else: whatever it is, all places of d_pages are seen, also where a captured call is replayed over longer sequences.
  *   Probabilities are fp32; they are rounded to the cache's type as factors of the values (the sum that divides them is of unrounded ones).
  *   n * m * heads <= 2^26; the launch is limited to 2^23 workgroups.
  * d_workspace: >= ivfpq_draft_attention_workspace_bytes(...) (may be 0), 256-byte aligned. */

@@ -550,7 +550,8 @@ def ivfpq_draft_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch
                           parents: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None, scale: Optional[float] = None,
                           max_places: Optional[int] = None, out: Optional[torch.Tensor] = None, with_lse: bool = False):
     """-> [n][m][heads][d] (with_lse: and lse [n][m][heads] fp32): attention of a pass's rows over the cache, whose last m places hold theirs.
-    scale: d ** -0.5 if None.  max_places: what no sequence exceeds with its rows (all of `pages` if None), best close to the longest."""
+    scale: d ** -0.5 if None.  max_places: about how many places the longest sequence has with its rows (as many as `pages` has if None); it
+    decides how the work is divided, not what is seen."""
     what = "ivfpq_draft_attention"
     _on_device(what, q, k_cache, v_cache, pages, lens, parents, counts, out)
     _, layout, n, page, held = _cache(what, k_cache, v_cache, pages, lens)

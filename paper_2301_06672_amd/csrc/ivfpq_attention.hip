@@ -757,7 +757,8 @@ int ivfpq_draft_attention(const void* d_q, int64_t q_stride, int32_t heads, int6
         if (rows > 1 && (q_stride < (int64_t)heads * d || out_stride < (int64_t)heads * d || q_stride % 8 || out_stride % 4))
             return fail(IVFPQ_EINVAL, "%s: a row stride below the row's values, or no multiple of 8 (queries) or 4 (output)", what);
         if ((uintptr_t)d_q % 16 || (uintptr_t)d_out % 8 || (uintptr_t)d_lse % 4) return fail(IVFPQ_EINVAL, "%s: queries are not aligned to 16 bytes, or the output not to 8", what);
-        const AttentionPlan plan = attention_plan(n, m, heads, kv_heads, d, max_places);
+        AttentionPlan plan = attention_plan(n, m, heads, kv_heads, d, max_places);
+        if (!tiles_numbered(n, (int64_t)max_pages * page)) plan.parts = 0;
         if (!fits_launch(n, kv_heads, plan)) return fail(IVFPQ_EUNSUPPORTED, "%s: n=%lld m=%d heads=%d kv_heads=%d: over 2^23 workgroups", what, (long long)n, m, heads, kv_heads);
         const size_t need = align_up((size_t)attention_scratch_bytes(n, kv_heads, d, plan));
         if (need) {
@@ -770,8 +771,8 @@ int ivfpq_draft_attention(const void* d_q, int64_t q_stride, int32_t heads, int6
         const size_t pieces = (size_t)attention_pieces(n, kv_heads, plan);
         in.norms = (float2*)(in.sums + pieces * d);        // d is a multiple of 8
         in.spans = (int2*)(in.norms + pieces);
-        // max_places bounds what is looked at: the table's end does
-        in.at.most = n_pages ? (int)std::min<int64_t>(max_pages, (max_places + page - 1) / page) : 0;
+        // what is looked at ends with the table, wherever max_places is: lengths may have grown since a call was captured
+        if (!n_pages) in.at.most = 0;
         return with_value_type(cache_dtype, [&](auto t) {
             using T = decltype(t);
             if constexpr (sizeof(T) == 4) return (int)IVFPQ_EINVAL;

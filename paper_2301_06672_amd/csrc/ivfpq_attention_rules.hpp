@@ -36,9 +36,12 @@ inline AttentionPlan attention_plan(int64_t n, int m, int heads, int kv_heads, i
     const int64_t groups = (int64_t)kv_heads * p.blocks, useful = n * max_places / (p.apart ? 128 : 256);
     const int64_t wanted = p.waves == 8 ? (n == 1 ? (256 + groups - 1) / groups : 512 / groups - n) : (512 + groups - 1) / groups;
     const int64_t parts = std::min<int64_t>({wanted, useful, kMostPartsEach * n});
-    p.parts = parts > n && n * (max_places / 32 + 2) < ((int64_t)1 << 31) ? (int)parts : 0;
+    p.parts = parts > n ? (int)parts : 0;
     return p;
 }
+
+// Whether the tiles of all sequences together, of as many places as the page table has, can be numbered by 31 bits: they are where they are dealt to parts.
+inline bool tiles_numbered(int64_t n, int64_t table_places) { return n * (table_places / 32 + 2) < ((int64_t)1 << 31); }
 
 // Scratch of divided places, in bytes: for every head, block and piece (a part's share of a sequence) the sums of d components for each column, then their
 // references and sums of weights; then the first and last part of every sequence and block.
