@@ -1,9 +1,10 @@
 // Drafted tokens against the model's logits: what ivfpq_verify_drafts does.
 //
 // A token is drawn by where a given number falls among sums of probabilities, and as many borders as there are tokens lie close together, so sums are of
-// 64 bits and their terms right to 10^-12: 2^y = 2^n 2^f with n the nearest whole number and a polynomial of degree 8 for 2^f, |f| <= 1/2
-// (interpolated at Chebyshev's points, off by 1.1 10^-12 at most).  A row is read once, in blocks whose largest logit and sum about it
-// are kept; where a token is drawn, the sums say in which block, and that block is read again.
+// 64 bits and their terms right to 1.1 10^-12.  A row is read once, in blocks whose largest logit and sum about it are kept; where a token is drawn, the
+// sums say in which block, and that block is read again.  Two exponentials, both with polynomials interpolated at Chebyshev's points: the terms of the blocks' sums are
+// 2^n 2^(i / 32) 2^(f / 32) with a table of 32 powers and degree 4 (off by 8 10^-14 at most), as there are many; everything else (what scales a
+// block's sum, the tokens of a block that is read again, a student's remainder) is 2^n 2^f with degree 8 (off by 1.1 10^-12).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -87,7 +88,7 @@ __device__ const double kExp2Table[32] = {
     0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0, 0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
     0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0, 0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0,
     0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0};
-// 2^(y / 32) in fewer instructions, right to 10^-13, from the nearest whole number of y and the rest: 2^(n + i / 32 + f / 32) with 2^(i / 32) from a table in
+// 2^(y / 32) in fewer instructions, right to 8 10^-14, from the nearest whole number of y and the rest: 2^(n + i / 32 + f / 32) with 2^(i / 32) from a table in
 // the LDS, n added to its exponent, and a polynomial of degree 4 for the rest, |f| <= 1/2.  An addition leaves the nearest whole number in the low bits.
 // The coefficients stay in vector registers: an operation takes one from a scalar register at most, and a copy of it costs as much as the operation.
 constexpr int kExp2Steps = 32;
@@ -662,10 +663,9 @@ int launch_verify(const VerifyIn& in, hipStream_t stream) {
     }
     hipLaunchKernelGGL((verify_chain_kernel<T>), dim3((unsigned)in.n), dim3(kWalkThreads), 0, stream, in);
     HIP_TRY(hipGetLastError());
-    if (in.m > 1) {                                    // else nothing was drafted.  A row of two at least: fewer than 2^26 waves
-        hipLaunchKernelGGL((left_sums_kernel<T>), dim3((unsigned)((in.n * in.left_blocks + kWaves - 1) / kWaves)), dim3(kSumThreads), 0, stream, in);
-        HIP_TRY(hipGetLastError());
-    }
+    // sequences of two rows at least, or nothing was drafted: fewer than 2^26 waves
+    hipLaunchKernelGGL((left_sums_kernel<T>), dim3((unsigned)((in.n * in.left_blocks + kWaves - 1) / kWaves)), dim3(kSumThreads), 0, stream, in);
+    HIP_TRY(hipGetLastError());
     hipLaunchKernelGGL((draw_left_kernel<T>), dim3((unsigned)in.n), dim3(64), 0, stream, in);
     HIP_TRY(hipGetLastError());
     return IVFPQ_OK;
