@@ -438,7 +438,8 @@ int ivfpq_cache_append(const void* d_q, int64_t q_stride, int32_t heads, const v
  *   fp32, may be NULL.
  *   max_places: about how many places the longest sequence has with its rows.  It decides how the work is divided and what workspace that needs, and nothing
  *   else: whatever it is, all places of d_pages are seen, also where a captured call is replayed over longer sequences.
- *   Probabilities are fp32; they are rounded to the cache's type as factors of the values (the sum that divides them is of unrounded ones).
+ *   Probabilities are fp32; they are rounded to the cache's type as factors of the values (the sum that divides them is of unrounded ones).  An infinity among the
+ *   values that a row sees makes its result infinite, or NaN where the weight rounds to 0 (in fp16 under 2^-31 of the largest).
  *   n * m * heads <= 2^26; the launch is limited to 2^23 workgroups.
  * d_workspace: >= ivfpq_draft_attention_workspace_bytes(...) (may be 0), 256-byte aligned. */
 size_t ivfpq_draft_attention_workspace_bytes(int64_t n, int32_t m, int32_t heads, int32_t kv_heads, int32_t d, int64_t max_places);

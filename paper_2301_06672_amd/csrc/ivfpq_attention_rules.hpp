@@ -28,11 +28,18 @@ inline AttentionPlan attention_plan(int64_t n, int m, int heads, int kv_heads, i
     p.waves = p.apart && columns > 128 && d <= 128 ? 8 : 4;
     p.tiles = p.apart ? (p.waves == 8 ? 2 : 1) : columns <= 16 ? 1 : 2;
     p.blocks = (int)((columns + p.columns() - 1) / p.columns());
-    // where sequences are too few to fill the GPU: parts for every CU twice over, of two tiles a wave at least.  They are equal whatever the lengths.
+    // Where sequences are too few to fill the GPU: some 512 parts of all heads and blocks together, of two tiles a wave at least, equal whatever the lengths.  A
+    // part that holds the end of a sequence is a piece more, so there are up to (parts + n) * groups.  (Workgroups that a CU has room for, by registers and LDS, of heads
+    // of up to 64, up to 128 and more components: shared columns of one tile 3, 2, 1, of two 2, 1; apart with four waves 3, 2, 1, with eight 1.  512 is not fitted to each
+    // of them: the 576 pieces of 8 rows of 8 sequences, two tiles shared, 48 us, come in over two rounds of 256; those of 12 rows, apart, 39 us, in one of 512 and a rest.)
     // (One row over 2,049 places, 32 heads of 128 over 8: parts of 128, 256 and 512 places take 10.1, 9.4 and 11.7 us, and joining them 6.5, 5.1 and 4.2.)
     // The kernel of eight waves leaves room for one workgroup on a CU: a part for each of one sequence, and of several, whose pieces differ, two rounds
     // of pieces (64 rows of 16 sequences of 2,111 to 8,191 places, 32 heads of 128 over 8: 384, 512, 640, 768, 1,024 pieces take 181, 161, 162, 170, 174 us,
     // and joining them 13, 16, 18, 22, 28).
+    // Where parts would be no more than sequences, from 64 sequences of single tokens and 32 of 64 rows on with 8 heads of keys, a workgroup has a whole sequence.  With
+    // lengths from the longest evenly down to a quarter of it nothing is lost: 64 rows of 31, 32 and 33 sequences up to 8,192 places 1.92, 1.64 and 1.79 ns a place,
+    // single tokens of 63, 64 and 80 up to 16,384 0.76, 0.77 and 0.78.  One long sequence among short ones is left to its own workgroups there: 65,536 places beside
+    // 1,000 each take 179 us with 31 sequences of 64 rows and 1,930 with 32, 120 us with 63 of single tokens and 1,400 with 64.
     const int64_t groups = (int64_t)kv_heads * p.blocks, useful = n * max_places / (p.apart ? 128 : 256);
     const int64_t wanted = p.waves == 8 ? (n == 1 ? (256 + groups - 1) / groups : 512 / groups - n) : (512 + groups - 1) / groups;
     const int64_t parts = std::min<int64_t>({wanted, useful, kMostPartsEach * n});
